@@ -415,6 +415,114 @@ int cf_ffn_set_spin_limit(cf_ffn t, int32_t spin_limit_us);
 /* Algorithmic HBM bytes of one call (the three matrices + z + out). */
 int64_t cf_ffn_algorithmic_bytes(const cf_ffn_config *cfg, int32_t batch);
 
+/* ------------------------------------------------------------------------------------------------
+ * Drafted tokens on a key/value cache: what a program that verifies several tokens per sequence at once (speculative
+ * decoding), fills a cache from a prompt or holds it in 8 bits runs around its own projections.
+ *
+ * The cache is that of cf_decode_block, [batch, n_kv_heads, max_seq, head_dim] for the keys and for the values, in one of
+ * three formats:
+ *   CF_CACHE_F16    fp16 (the tensors that cf_decode_block and cf_decode_layer take; no scales)
+ *   CF_CACHE_E4M3   8-bit floats (OCP e4m3: 448 is the largest) and one fp32 scale for every cached row of a head,
+ *   CF_CACHE_INT8   8-bit integers (-127..127)                  scales [batch, n_kv_heads, max_seq]; a value is code * scale
+ * A row (head_dim fp16 values) is held in 8 bits as  scale = top / Q  and  code = x * Q / top  rounded to the nearest code, ties
+ * to even, where top is the row's largest magnitude and Q = 448 or 127; the code is the correctly rounded one.  A row of zeros has
+ * scale 0 and codes 0; a row that holds an infinity or a NaN has scale NaN and codes 0, so that all of it reads back as NaN.
+ */
+enum { CF_CACHE_F16 = 0, CF_CACHE_E4M3 = 1, CF_CACHE_INT8 = 2 };
+typedef struct cf_cache_config {
+    int32_t n_q_heads, n_kv_heads;  /* n_q_heads % n_kv_heads == 0: query head i uses KV head i / (n_q_heads / n_kv_heads) */
+    int32_t head_dim;               /* 64 or 128 */
+    int32_t max_batch, max_seq;     /* largest batch of a call; rows of a head's slice of the cache */
+    int32_t format;                 /* CF_CACHE_* */
+    float   rope_base;
+} cf_cache_config;
+
+/* DEVICE pointers of a cache, k and v 16-byte aligned; the scales (4-byte aligned) are not read with CF_CACHE_F16 and may be NULL
+ * then.  The four buffers must not overlap. */
+typedef struct cf_cache {
+    void *k, *v;
+    float *k_scale, *v_scale;
+} cf_cache;
+
+/* New tokens behind the cached ones.  Batch row b has row_len[b] cached tokens (cache rows 0 .. row_len[b] - 1) and n_b =
+ * row_tokens[b] new ones, whose keys and values have the rows row_len[b] + t, t = 0 .. n_b - 1.  A call's tensors have `tokens`
+ * tokens for every batch row; those from n_b on are padding, neither read nor written.  Token t has the position
+ * row_len[b] + depth[t] and sees (cf_tree_attend) the cached rows and the new tokens u < n_b whose bit u is set in its mask: bit
+ * u % 64 of word u / 64 of tree[t][(tokens + 63) / 64].  A token sees itself only if its own bit is set.  Without masks a token
+ * sees the new tokens 0 .. t (a chain). */
+typedef struct cf_draft {
+    int32_t tokens;             /* >= 1 */
+    int32_t max_len;            /* HOST bound of row_len's entries, max_len + tokens <= max_seq */
+    const int32_t *row_len;     /* DEVICE [batch], or NULL: max_len for every batch row */
+    const int32_t *row_tokens;  /* DEVICE [batch], or NULL: `tokens` for every batch row */
+    const int32_t *depth;       /* DEVICE [tokens], or NULL: t */
+    const uint64_t *tree;       /* DEVICE [tokens][(tokens + 63) / 64], or NULL: a chain */
+    int32_t per_row;            /* not 0: depth and tree (where given) have a leading dimension [batch] */
+} cf_draft;
+/* The DEVICE arrays are read by the kernels (earlier work on the stream may write them).  Entries outside 0..max_len (row_len) and
+ * 0..tokens (row_tokens) are clamped.  The structs themselves are HOST memory and read during the call only.
+ *
+ * All calls below are asynchronous on `stream`, allocate nothing, wait for nothing and can be captured and replayed.  CF_EINVAL: a
+ * null or misaligned pointer, a batch outside 1..max_batch, a cf_draft outside the limits above, a malformed cf_cache_config;
+ * CF_EUNSUPPORTED: another head_dim, a head's slice of the cache of 2 GiB or more, more than 65535 heads in a call
+ * (batch * n_kv_heads); CF_EHIP: the launch failed.
+ *
+ * cf_cache_append: qkv [batch, tokens, (n_q + 2 n_kv) * head_dim] fp16, columns ordered as those of W_qkv in cf_decode_block (the
+ *   product of the tokens' hidden states with it); queries and keys are rotated for their positions as in cf_decode_block (angles
+ *   and products in fp64, one rounding to fp16), q_out [batch, tokens, n_q, head_dim] fp16 receives the queries, the cache rows
+ *   row_len[b] + t the keys and values.  Any number of tokens that the cache holds: a prompt, a tree, one token.  q_out must not
+ *   overlap qkv.
+ * cf_cache_read: rows first .. first + rows - 1 of every head's slice as fp16, k_out and v_out [batch, n_kv, rows, head_dim]; 8-bit
+ *   values are rounded once more, from the fp32 product code * scale.  rows 0 does nothing.
+ * cf_cache_keep: after verification, row row_len[b] + i of every head's slice becomes what row row_len[b] + kept[b][i] was, for
+ *   i < n_kept[b] (keys, values and scales; all rows are read before one is written); the rows behind stay as they were.  kept: DEVICE [batch,
+ *   tokens] int32, entries clamped into 0..n_b - 1; they may come in any order and more than once; n_kept: DEVICE [batch] int32,
+ *   clamped into 0..n_b.  new_len: DEVICE [batch] int32 that receives row_len[b] + n_kept[b], or NULL; it must not overlap the
+ *   other arrays.  draft's depth, tree and per_row are not looked at; tokens at most 256 (CF_EUNSUPPORTED).
+ */
+int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, const cf_cache *cache, const cf_draft *draft,
+                    void *q_out, void *stream);
+int cf_cache_read(const cf_cache_config *cfg, int32_t batch, const cf_cache *cache, int32_t first, int32_t rows, void *k_out,
+                  void *v_out, void *stream);
+int cf_cache_keep(const cf_cache_config *cfg, int32_t batch, const cf_cache *cache, const cf_draft *draft, const int32_t *kept,
+                  const int32_t *n_kept, int32_t *new_len, void *stream);
+
+/*
+ * Attention of drafted tokens over the cache.  For query head h of token t of batch row b, over the keys j that the token sees:
+ *
+ *   s_j = q . k_j / sqrt(head_dim);   score_cap > 0: s_j <- score_cap * tanh(s_j / score_cap);
+ *   slopes != NULL: s_j <- s_j - slopes[h] * (position of t - position of j);   window > 0: j only where that distance is < window
+ *   out = sum_j softmax(s)_j v_j
+ *
+ * q [batch, tokens, n_q, head_dim] fp16, rotated (q_out of cf_cache_append); the drafted tokens' keys and values are in the cache
+ * already; the position of cached row j is j, that of a drafted token as above.  slopes: DEVICE [n_q] fp32, finite, 4-byte aligned, or NULL.
+ * out [batch, tokens, n_q, head_dim] fp16, must not overlap q: rows of padding stay as they were; a token that sees no key, or
+ * only keys with a score of minus infinity, gets zeros.  What a token does not see does not enter its result, whatever it holds
+ * (NaN and infinities among it).  Scores, softmax statistics and sums are fp32.  With the same row_len, row_tokens, max_len and batch the same
+ * inputs give the same bits; otherwise the last bits may depend on how the cached rows are divided.
+ *
+ * cf_tree_create: a handle on the current device for calls of up to max_tokens tokens (1..256) with this score_cap (0: none) and
+ *   window (0: none).  Allocates a workspace for partial results (synchronous).  CF_EINVAL also for a negative or non-finite
+ *   score_cap and a negative window.  A handle must not be used from two streams at the same time, nor two captured graphs with
+ *   calls on one handle replayed at the same time, and only while its device is the current one (CF_EINVAL).
+ * cf_tree_set_splits: upper limit on the number of parts a sequence's keys are divided into; 0 = chosen by the library.  For
+ *   tests and measurements; CF_EINVAL outside 0..64.
+ * cf_tree_algorithmic_bytes: HBM bytes a call cannot do without with `len` cached rows in every batch row (keys and values once, q, out).
+ */
+typedef struct cf_tree_config {
+    cf_cache_config cache;
+    int32_t max_tokens;
+    float score_cap;
+    int32_t window;
+} cf_tree_config;
+typedef struct cf_tree_s *cf_tree;
+int cf_tree_create(const cf_tree_config *cfg, cf_tree *out);
+int cf_tree_destroy(cf_tree t);
+int cf_tree_attend(cf_tree t, int32_t batch, const void *q, const cf_cache *cache, const cf_draft *draft, const float *slopes,
+                   void *out, void *stream);
+int cf_tree_set_splits(cf_tree t, int32_t max_splits);
+int64_t cf_tree_algorithmic_bytes(const cf_tree_config *cfg, int32_t batch, int32_t tokens, int32_t len);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,7 +25,9 @@ EXPORTED_SYMBOLS = ("cf_create", "cf_destroy", "cf_decode_block", "cf_decode_blo
                     "cf_splithead_create", "cf_splithead_destroy", "cf_splithead_pack", "cf_splithead_decode",
                     "cf_splithead_status", "cf_splithead_set_spin_limit",
                     "cf_ffn_create", "cf_ffn_destroy", "cf_ffn_decode", "cf_ffn_status", "cf_ffn_set_spin_limit",
-                    "cf_ffn_algorithmic_bytes")
+                    "cf_ffn_algorithmic_bytes",
+                    "cf_cache_append", "cf_cache_read", "cf_cache_keep",
+                    "cf_tree_create", "cf_tree_destroy", "cf_tree_attend", "cf_tree_set_splits", "cf_tree_algorithmic_bytes")
 
 CF_FLAG_DEBUG_EXPORT = 1
 
@@ -49,6 +51,29 @@ class FfnConfig(ctypes.Structure):
 
 FFN_SILU = 0
 FFN_GELU = 1
+
+
+class CacheConfig(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("max_batch", ctypes.c_int32), ("max_seq", ctypes.c_int32), ("format", ctypes.c_int32),
+                ("rope_base", ctypes.c_float)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class Draft(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("max_len", ctypes.c_int32), ("row_len", ctypes.c_void_p),
+                ("row_tokens", ctypes.c_void_p), ("depth", ctypes.c_void_p), ("tree", ctypes.c_void_p),
+                ("per_row", ctypes.c_int32)]
+
+
+class TreeConfig(ctypes.Structure):
+    _fields_ = [("cache", CacheConfig), ("max_tokens", ctypes.c_int32), ("score_cap", ctypes.c_float), ("window", ctypes.c_int32)]
+
+
+CACHE_F16, CACHE_E4M3, CACHE_INT8 = 0, 1, 2
 
 
 class CfError(RuntimeError):
@@ -125,6 +150,19 @@ def load_library():
         lib.cf_ffn_algorithmic_bytes.argtypes = [ctypes.POINTER(FfnConfig), i32]
         lib.cf_ffn_algorithmic_bytes.restype = ctypes.c_int64
         for name in ("cf_ffn_create", "cf_ffn_destroy", "cf_ffn_decode", "cf_ffn_status", "cf_ffn_set_spin_limit"):
+            getattr(lib, name).restype = ctypes.c_int
+        cfg_p, cache_p, draft_p = ctypes.POINTER(CacheConfig), ctypes.POINTER(Cache), ctypes.POINTER(Draft)
+        lib.cf_cache_append.argtypes = [cfg_p, i32, vp, cache_p, draft_p, vp, vp]
+        lib.cf_cache_read.argtypes = [cfg_p, i32, cache_p, i32, i32, vp, vp, vp]
+        lib.cf_cache_keep.argtypes = [cfg_p, i32, cache_p, draft_p, vp, vp, vp, vp]
+        lib.cf_tree_create.argtypes = [ctypes.POINTER(TreeConfig), ctypes.POINTER(vp)]
+        lib.cf_tree_destroy.argtypes = [vp]
+        lib.cf_tree_attend.argtypes = [vp, i32, vp, cache_p, draft_p, vp, vp, vp]
+        lib.cf_tree_set_splits.argtypes = [vp, i32]
+        lib.cf_tree_algorithmic_bytes.argtypes = [ctypes.POINTER(TreeConfig), i32, i32, i32]
+        lib.cf_tree_algorithmic_bytes.restype = ctypes.c_int64
+        for name in ("cf_cache_append", "cf_cache_read", "cf_cache_keep", "cf_tree_create", "cf_tree_destroy", "cf_tree_attend",
+                     "cf_tree_set_splits"):
             getattr(lib, name).restype = ctypes.c_int
         lib.cf_decode_stack.argtypes = [vp, i32, i32, vp, ctypes.POINTER(vp), ctypes.c_float, i32, i32, ctypes.POINTER(vp),
                                         ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(vp), i32, vp, vp]
@@ -432,6 +470,93 @@ class SplitHeadBlock:
     def close(self):
         if self._h:
             self._lib.cf_splithead_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def cache_pointers(k, v, k_scale=0, v_scale=0) -> Cache:
+    """The buffers of a key/value cache (cf_cache) from their device addresses; the scales are needed with 8-bit formats."""
+    return Cache(k or None, v or None, k_scale or None, v_scale or None)
+
+
+def draft(tokens, max_len, row_len=0, row_tokens=0, depth=0, tree=0, per_row=False) -> Draft:
+    """New tokens behind the cached ones (cf_draft); row_len, row_tokens, depth, tree: device addresses, 0 for none."""
+    return Draft(tokens, max_len, row_len or None, row_tokens or None, depth or None, tree or None, int(per_row))
+
+
+class KvCache:
+    """Calls on a key/value cache in fp16 or 8 bits (cf_cache_*).  Tensors are raw device addresses; `cache` and `draft` come
+    from cache_pointers() and draft()."""
+
+    def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, format, rope_base):
+        self._lib = load_library()
+        self.cfg = CacheConfig(n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, format, rope_base)
+
+    def _check(self, rc):
+        if rc != 0:
+            raise CfError(rc, self._lib.cf_strerror(rc).decode())
+
+    def append(self, batch, qkv, cache, draft, q_out, stream=0):
+        rc = self._lib.cf_cache_append(self.cfg, batch, qkv, cache, draft, q_out, stream)
+        if rc != 0:
+            self._check(rc)
+
+    def append_rc(self, batch, qkv, cache, draft, q_out, stream=0) -> int:
+        return int(self._lib.cf_cache_append(self.cfg, batch, qkv, cache, draft, q_out, stream))
+
+    def read(self, batch, cache, first, rows, k_out, v_out, stream=0):
+        rc = self._lib.cf_cache_read(self.cfg, batch, cache, first, rows, k_out, v_out, stream)
+        if rc != 0:
+            self._check(rc)
+
+    def read_rc(self, batch, cache, first, rows, k_out, v_out, stream=0) -> int:
+        return int(self._lib.cf_cache_read(self.cfg, batch, cache, first, rows, k_out, v_out, stream))
+
+    def keep(self, batch, cache, draft, kept, n_kept, new_len=0, stream=0):
+        rc = self._lib.cf_cache_keep(self.cfg, batch, cache, draft, kept, n_kept, new_len, stream)
+        if rc != 0:
+            self._check(rc)
+
+    def keep_rc(self, batch, cache, draft, kept, n_kept, new_len=0, stream=0) -> int:
+        return int(self._lib.cf_cache_keep(self.cfg, batch, cache, draft, kept, n_kept, new_len, stream))
+
+
+class TreeAttention:
+    """Handle of the attention of drafted tokens over a cache (cf_tree_*).  Arguments as for KvCache."""
+
+    def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, format, rope_base, max_tokens, score_cap=0.0, window=0):
+        self._lib = load_library()
+        self.cfg = TreeConfig(CacheConfig(n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, format, rope_base), max_tokens,
+                              score_cap, window)
+        self._h = ctypes.c_void_p()
+        self._check(self._lib.cf_tree_create(ctypes.byref(self.cfg), ctypes.byref(self._h)))
+
+    def _check(self, rc):
+        if rc != 0:
+            raise CfError(rc, self._lib.cf_strerror(rc).decode())
+
+    def attend(self, batch, q, cache, draft, slopes, out, stream=0):
+        rc = self._lib.cf_tree_attend(self._h, batch, q, cache, draft, slopes, out, stream)
+        if rc != 0:
+            self._check(rc)
+
+    def attend_rc(self, batch, q, cache, draft, slopes, out, stream=0) -> int:
+        return int(self._lib.cf_tree_attend(self._h, batch, q, cache, draft, slopes, out, stream))
+
+    def set_splits(self, max_splits):
+        self._check(self._lib.cf_tree_set_splits(self._h, max_splits))
+
+    def algorithmic_bytes(self, batch, tokens, length) -> int:
+        return int(self._lib.cf_tree_algorithmic_bytes(ctypes.byref(self.cfg), batch, tokens, length))
+
+    def close(self):
+        if self._h:
+            self._lib.cf_tree_destroy(self._h)
             self._h = ctypes.c_void_p()
 
     def __del__(self):

@@ -44,5 +44,25 @@ __device__ __forceinline__ void rope_cos_sin(int pos, double inv_freq, float &co
     sin_out = (float)sv;
 }
 
+// cos and sin of pos * inv_freq in fp64, errors below 2^-51: the angle less the nearest multiple of pi / 2 (taken off in two parts),
+// the Taylor series of both up to a remainder of 2^-54 at pi / 4, and the quadrant.
+__device__ __forceinline__ void rope_cos_sin64(double pos, double inv_freq, double &cos_out, double &sin_out)
+{
+    const double ang = pos * inv_freq;
+    const double k = rint(ang * 0.63661977236758134308);              // 2/pi
+    const double r = fma(-k, 6.12323399573676603587e-17, fma(-k, 1.57079632679489655800e+00, ang)), r2 = r * r;
+    double s = 0.0, c = 0.0;
+#pragma unroll
+    for (int n = 16; n >= 2; n -= 2) {                                // s = 1 - r2 / 2 3 (1 - r2 / 4 5 (...)), c = 1 - r2 / 1 2 (...)
+        s = fma(-(1.0 / (n * (n + 1))) * r2, s, -(1.0 / (n * (n + 1))) * r2);
+        c = fma(-(1.0 / (n * (n - 1))) * r2, c, -(1.0 / (n * (n - 1))) * r2);
+    }
+    const double sr = fma(s, r, r), cr = 1.0 + c;
+    const int q = (int)((long long)k & 3);
+    const double sv = q & 1 ? cr : sr, cv = q & 1 ? sr : cr;
+    sin_out = q & 2 ? -sv : sv;
+    cos_out = (q + 1) & 2 ? -cv : cv;
+}
+
 }  // namespace cf
 #endif

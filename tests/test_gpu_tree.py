@@ -1,0 +1,469 @@
+"""cf_tree_attend against oracle/draft_block.py, through the C ABI, at the sizes and masks where it can go wrong; tolerances as derived
+in draft_cases.bound."""
+import numpy as np
+import pytest
+
+from draft_cases import FORMATS, bound, bytes_code, cache_values, mask_words, random_tree
+from oracle import draft_block as orc
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def _dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+class Case:
+    """Inputs of one call on the host and on the GPU."""
+
+    def __init__(self, fmt, nq, nkv, d, lens, T, counts=None, chain=False, per_row=True, cap=0.0, window=0, slopes=False, seed=0,
+                 max_len=None, extra=5, max_tokens=None, q_size=1.0, mask=None, depth=None):
+        import paper_2508_18850_amd as lib
+        self.lib, self.fmt, self.nq, self.nkv, self.d, self.T = lib, fmt, nq, nkv, d, T
+        self.B, self.lens = len(lens), lens
+        self.counts = [T] * self.B if counts is None else counts
+        self.ragged = counts is not None
+        self.max_len = max(lens) if max_len is None else max_len
+        self.rows = self.max_len + T + extra
+        rng = np.random.default_rng(seed + 1000 * T + sum(lens))
+        self.cap, self.window = cap, window
+        self.slopes = (2.0 ** (-8.0 * (np.arange(nq) + 1) / nq)).astype(np.float32) if slopes else None
+        self.q = (q_size * rng.standard_normal((self.B, T, nq, d))).astype(np.float16)
+        trees = [random_tree(rng, T, chain) for _ in range(self.B)]
+        if not per_row:
+            trees = trees[:1] * self.B
+        self.depth = np.stack([t[0] for t in trees]) if depth is None else depth
+        self.mask = np.stack([t[1] for t in trees]) if mask is None else mask
+        self.chain, self.per_row = chain, per_row
+        self.k, self.ks, self.kv = cache_values(rng, (self.B, nkv, self.rows, d), fmt)
+        self.v, self.vs, self.vv = cache_values(rng, (self.B, nkv, self.rows, d), fmt)
+        self.tree = lib.TreeAttention(nq, nkv, d, self.B, self.rows, FORMATS[fmt], 10000.0, max_tokens or T, cap, window)
+
+    def poison_rest(self):
+        """What lies behind the new tokens of a row is not to be read: NaN there (fp16), or a NaN scale."""
+        for b in range(self.B):
+            end = self.lens[b] + self.counts[b]
+            if self.fmt == "f16":
+                self.k[b, :, end:], self.v[b, :, end:] = np.nan, np.nan
+            else:
+                self.ks[b, :, end:], self.vs[b, :, end:] = np.nan, np.nan
+
+    def upload(self):
+        self.t = {n: _dev(x) for n, x in (("k", self.k), ("v", self.v), ("q", self.q))}
+        for n, x in (("ks", self.ks), ("vs", self.vs), ("slopes", self.slopes)):
+            self.t[n] = _dev(x) if x is not None else None
+        self.t["lens"], self.t["counts"] = _dev(np.array(self.lens, np.int32)), _dev(np.array(self.counts, np.int32))
+        pick = slice(None) if self.per_row else 0
+        self.t["depth"], self.t["mask"] = _dev(self.depth[pick].astype(np.int32)), _dev(mask_words(self.mask[pick]).view(np.int64))
+        p = lambda n: self.t[n].data_ptr() if self.t[n] is not None else 0  # noqa: E731
+        self.cache = self.lib.cache_pointers(p("k"), p("v"), p("ks"), p("vs"))
+        same = len(set(self.lens)) == 1 and self.max_len == self.lens[0]
+        self.draft = self.lib.draft(self.T, self.max_len, row_len=0 if same else p("lens"), row_tokens=p("counts") if self.ragged else 0,
+                                    depth=0 if self.chain else p("depth"), tree=0 if self.chain else p("mask"), per_row=self.per_row)
+        self.out = torch.full((self.B, self.T, self.nq, self.d), 7.0, dtype=torch.float16, device="cuda")
+
+    def call(self, stream=None):
+        self.tree.attend(self.B, self.t["q"].data_ptr(), self.cache, self.draft, self.t["slopes"].data_ptr() if self.slopes is not None else 0,
+                         self.out.data_ptr(), _stream() if stream is None else stream)
+
+    def run(self):
+        self.upload()
+        self.call()
+        torch.cuda.synchronize()
+        return self.out.cpu().numpy()
+
+    def want(self):
+        return orc.attend(self.q, self.kv, self.vv, self.lens, self.counts, self.depth, self.mask, self.slopes, self.cap, self.window)
+
+    def check(self, got=None):
+        got = self.run() if got is None else got
+        out, size, reach = self.want()
+        pad = np.isnan(out).all(-1)
+        for b in range(self.B):
+            pad[b, :self.counts[b]] = False
+        assert (got[pad] == 7.0).all(), "padding was written"
+        slope_reach = 0.0 if self.slopes is None else float(self.slopes.max()) * (self.max_len + self.T)
+        tol = bound(out, size, reach, self.d, max(self.lens) + self.T, slope_reach)
+        ok = np.broadcast_to(~pad[..., None], out.shape)
+        # fp16 ends at 65504: from 65520 on the nearest one is infinite.  What is within its bound of that may be either.
+        far = ok & (np.abs(out) - np.where(ok, tol, 0) >= 65520)
+        assert np.array_equal(got[far], np.sign(out[far]) * np.inf)
+        near = ok & ~far & (np.abs(out) + np.where(ok, tol, 0) >= 65520) & np.isinf(got)
+        assert np.array_equal(np.sign(got[near]), np.sign(out[near]))
+        ok = ok & ~far & ~near
+        assert np.isfinite(got[ok]).all()
+        err = np.abs(got[ok].astype(np.float64) - out[ok])
+        worst = (err / tol[ok]).max() if err.size else 0.0
+        rel = np.sqrt((err ** 2).sum() / max((out[ok] ** 2).sum(), 1e-30)) if err.size else 0.0
+        print("   worst error / bound %.3f, relative %.2e" % (worst, rel), flush=True)
+        assert worst <= 1.0, worst
+        return got
+
+
+def _say(*what):
+    print("attend:", *what, flush=True)
+
+
+# lengths around the tiles of 32 and the parts, drafts around the tiles of 16 rows, one and several row blocks
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("L", [0, 1, 15, 31, 32, 33, 63, 64, 127, 250, 511])
+def test_lengths(fmt, L):
+    _say(fmt, "L", L)
+    Case(fmt, 4, 2, 64, [L], 3, seed=1).check()
+    Case(fmt, 4, 1, 128, [L], 5, seed=2).check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [1, 2, 7, 16, 17, 31, 33, 63, 64, 65, 100, 128, 256])
+def test_drafts(fmt, d, T):
+    _say(fmt, "d", d, "T", T)
+    c = Case(fmt, 2, 1, d, [75], T, seed=3)
+    c.poison_rest()
+    c.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("nq,nkv", [(1, 1), (3, 1), (5, 5), (8, 1), (16, 1), (12, 4), (64, 8), (24, 1)], ids=str)
+def test_heads(fmt, nq, nkv):
+    _say(fmt, "heads", nq, nkv)
+    for T in (1, 6):
+        Case(fmt, nq, nkv, 64 if nq % 2 else 128, [90], T, seed=4).check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("per_row", [True, False])
+def test_ragged_batches(fmt, per_row):
+    """Lengths and counts of their own, a row without cached tokens, one without new ones, a bound above all lengths; what lies
+    behind is NaN."""
+    _say(fmt, "ragged", per_row)
+    c = Case(fmt, 8, 2, 128, [300, 0, 77, 140], 9, counts=[9, 4, 0, 1], per_row=per_row, seed=5, max_len=333)
+    c.poison_rest()
+    c.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("cap,window,slopes", [(5.0, 0, False), (0.0, 40, False), (0.0, 0, True), (20.0, 100, True), (0.0, 1, False),
+                                               (0.0, 10000, True)], ids=str)
+def test_forms_of_the_score(fmt, cap, window, slopes):
+    _say(fmt, "cap", cap, "window", window, "slopes", slopes)
+    Case(fmt, 6, 2, 64, [190, 23], 12, cap=cap, window=window, slopes=slopes, seed=6, q_size=3.0).check()
+    Case(fmt, 4, 2, 128, [333], 70, chain=True, cap=cap, window=window, slopes=slopes, seed=7).check()
+    Case(fmt, 8, 1, 128, [0, 65], 4, counts=[4, 2], cap=cap, window=window, slopes=slopes, seed=8).check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_chain_needs_no_masks(fmt):
+    c = Case(fmt, 4, 2, 64, [50, 20], 20, chain=True, seed=9)
+    got = c.run()
+    c.chain = False                                             # the same tree as masks and depths
+    assert np.array_equal(got, c.run())
+    c.check(got)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_rows_that_see_nothing(fmt):
+    """An empty cache and empty masks; a window that reaches no key; depths without order."""
+    mask = np.zeros((2, 5, 5), bool)
+    mask[:, 2, 4] = mask[:, 3, 0] = True
+    depth = np.array([[0, 3, 1, 7, 2]] * 2, np.int32)
+    got = Case(fmt, 2, 1, 64, [0, 3], 5, mask=mask, depth=depth, seed=10).check()
+    assert not got[0, [0, 1, 4]].any() and got[1].any(-1).all()
+    got = Case(fmt, 2, 1, 128, [6, 40], 5, mask=mask, depth=depth, window=2, seed=11).check()
+    assert not got[0, 1].any() and not got[1, 1].any() and got[0, 0].any()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("T", [6, 40])
+def test_masked_rows_may_hold_anything(d, what, T):
+    """A drafted token's key and value are NaN or infinite: whoever does not see it gets the result without it, to the bit.  And a
+    cached row outside the window of some tokens."""
+    _say("masked", what, T, d)
+    depth, mask = random_tree(np.random.default_rng(3), T)
+    mask[:, 3] = False
+    mask[3, 3] = mask[5, 3] = True
+    c = Case("f16", 4, 2, d, [70], T, mask=mask[None], depth=depth[None], seed=12)
+    clean = c.run()
+    c.k[0, :, 73], c.v[0, :, 73] = what, what
+    got = c.run()
+    blind = [t for t in range(T) if not mask[t, 3]]
+    assert np.array_equal(got[:, blind], clean[:, blind])
+    assert not np.isfinite(got[0, [3, 5]]).any()
+    chain = Case("f16", 2, 1, d, [50], T, chain=True, window=10, seed=13)
+    clean = chain.run()
+    chain.k[0, :, 42], chain.v[0, :, 42] = what, what           # distance of token t: 8 + t
+    got = chain.run()
+    assert np.array_equal(got[0, 2:], clean[0, 2:]) and not np.isfinite(got[0, :2]).any()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_masked_rows_with_nan_scales(fmt):
+    depth, mask = random_tree(np.random.default_rng(4), 20)
+    mask[:, 7] = False
+    mask[7, 7] = True
+    c = Case(fmt, 4, 2, 128, [70], 20, mask=mask[None], depth=depth[None], seed=14)
+    clean = c.run()
+    c.ks[0, :, 77], c.vs[0, :, 77] = np.nan, np.nan
+    got = c.run()
+    blind = [t for t in range(20) if t != 7]
+    assert np.array_equal(got[:, blind], clean[:, blind]) and np.isnan(got[0, 7]).all()
+
+
+def test_visible_infinities():
+    """A value row with an infinity gives that infinity to whoever sees it, in its dimension only."""
+    c = Case("f16", 2, 1, 64, [40], 3, chain=True, seed=15)
+    clean = c.run()
+    c.v[0, 0, 11, 5], c.v[0, 0, 41, 9] = np.inf, -np.inf
+    got = c.run()
+    assert (got[0, :, :, 5] == np.inf).all() and (got[0, 1:, :, 9] == -np.inf).all() and np.isfinite(got[0, 0, :, 9]).all()
+    keep = [i for i in range(64) if i not in (5, 9)]
+    assert np.array_equal(got[..., keep], clean[..., keep])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("size", [1e-6, 1e-3, 100.0])
+def test_value_rows_of_any_size(fmt, size):
+    """Scales of the value rows over many orders of magnitude, small rows first and last."""
+    c = Case(fmt, 4, 1, 128, [200], 4, seed=16)
+    factor = np.float32(size) * np.exp(np.linspace(-6, 6, c.rows)).astype(np.float32)
+    for order in (1, -1):
+        c.vs = c.vs * 0 + np.abs(np.random.default_rng(1).standard_normal(c.vs.shape).astype(np.float32) * factor[::order])
+        c.vv = bytes_code(c.v, fmt) * c.vs.astype(np.float64)[..., None]
+        c.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("q_size", [30.0, 1000.0])
+def test_peaked_and_growing_scores(fmt, q_size):
+    """Scores of hundreds and more, growing along the keys, so that the running maximum moves all the time."""
+    c = Case(fmt, 4, 1, 64, [257], 3, seed=17, q_size=q_size)
+    c.check()
+    if fmt == "f16":
+        c.q[:] = np.abs(c.q)
+        c.k[:] = (np.abs(c.k) * np.linspace(0, 1, c.rows)[:, None]).astype(np.float16)
+        c.kv = c.k.astype(np.float64)
+        c.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T", [1, 5, 40])
+def test_splits_do_not_matter(fmt, T):
+    """Any limit on the parts: within the bound, and the same bits again."""
+    c = Case(fmt, 8, 2, 128, [1000, 333], T, seed=18)
+    for splits in (1, 2, 3, 7, 64, 0):
+        c.tree.set_splits(splits)
+        _say(fmt, "splits", splits, "T", T)
+        first = c.run()
+        c.check(first)
+        c.out.fill_(7.0)
+        c.call()
+        torch.cuda.synchronize()
+        assert np.array_equal(first, c.out.cpu().numpy())
+
+
+def test_long_cache():
+    """Many parts with many keys each, the product of the largest shape's heads; checked on three heads."""
+    for fmt, T in (("e4m3", 1), ("int8", 9), ("f16", 33)):
+        _say(fmt, "long", T)
+        c = Case(fmt, 8, 1, 128, [20000], T, seed=19)
+        c.check()
+
+
+def test_one_handle_for_calls_of_different_sizes():
+    big = Case("f16", 8, 2, 64, [700, 100], 40, seed=20)
+    small = Case("f16", 8, 2, 64, [30, 9], 2, seed=21, max_tokens=40, extra=big.rows - 32)
+    assert small.rows == big.rows
+    small.tree.close()
+    small.tree = big.tree
+    for c in (big, small, big):
+        c.check()
+
+
+@pytest.mark.parametrize("fmt,T", [("f16", 1), ("int8", 40)], ids=str)
+def test_captured_and_replayed(fmt, T):
+    """Three replays with eager calls and changed lengths between them: the lengths are read on the device."""
+    c = Case(fmt, 8, 2, 128, [900, 500], T, seed=22, max_len=901)
+    eager = c.run()
+    s = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        c.call(torch.cuda.current_stream().cuda_stream)
+    for replay in range(3):
+        c.out.fill_(7.0)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(c.out.cpu().numpy(), eager), replay
+        c.call()
+    c.t["lens"].copy_(_dev(np.array([321, 0], np.int32)))
+    g.replay()
+    torch.cuda.synchronize()
+    c.lens = [321, 0]
+    c.check(c.out.cpu().numpy())
+
+
+def test_a_stream_of_its_own():
+    c = Case("e4m3", 8, 2, 64, [300], 4, seed=23)
+    want = c.run()
+    s = torch.cuda.Stream()
+    c.out.fill_(7.0)
+    s.wait_stream(torch.cuda.current_stream())
+    c.call(s.cuda_stream)
+    s.synchronize()
+    assert np.array_equal(want, c.out.cpu().numpy())
+
+
+def test_two_handles_on_two_streams():
+    """Workspaces belong to handles: two of them at once do not disturb each other."""
+    cases = [Case("f16", 8, 2, 128, [4000], 16, seed=24 + i) for i in range(2)]
+    want = [c.run() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    for c in cases:
+        c.out.fill_(7.0)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s in zip(cases, streams):
+            c.call(s.cuda_stream)
+    torch.cuda.synchronize()
+    for c, w in zip(cases, want):
+        assert np.array_equal(c.out.cpu().numpy(), w)
+
+
+def test_refusals():
+    import paper_2508_18850_amd as lib
+    tree = lib.TreeAttention(4, 2, 64, 2, 100, 1, 10000.0, 8)
+    buf = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    p = buf.data_ptr()
+    cache = lib.cache_pointers(p, p, p, p)
+    ok = lib.draft(8, 50)
+    bad = lambda rc: rc == -1  # noqa: E731
+    assert bad(tree.attend_rc(0, p, cache, ok, 0, p)) and bad(tree.attend_rc(3, p, cache, ok, 0, p))
+    assert bad(tree.attend_rc(1, 0, cache, ok, 0, p)) and bad(tree.attend_rc(1, p, cache, ok, 0, 0))
+    assert bad(tree.attend_rc(1, p + 8, cache, ok, 0, p)) and bad(tree.attend_rc(1, p, cache, ok, 0, p + 2)) and bad(tree.attend_rc(1, p, cache, ok, p + 2, p))
+    assert bad(tree.attend_rc(1, p, cache, ok, 0, p)) and bad(tree.attend_rc(1, p, cache, ok, 0, p + 8 * 4 * 64 * 2 - 16))     # out on q
+    for draft in (lib.draft(9, 50), lib.draft(0, 50), lib.draft(8, 93), lib.draft(8, -1), lib.draft(8, 50, row_len=p + 1),
+                  lib.draft(8, 50, row_tokens=p + 1), lib.draft(8, 50, depth=p + 2), lib.draft(8, 50, tree=p + 4)):
+        assert bad(tree.attend_rc(1, p, cache, draft, 0, p + 4096)), draft
+    for k, v, ks, vs in ((0, p, p, p), (p, 0, p, p), (p, p, 0, p), (p, p, p, 0), (p + 4, p, p, p), (p, p, p + 1, p)):
+        assert bad(tree.attend_rc(1, p, lib.cache_pointers(k, v, ks, vs), ok, 0, p + 4096))
+    for n in (-1, 65):
+        with pytest.raises(lib.CfError):
+            tree.set_splits(n)
+    torch.cuda.synchronize()
+
+
+# ---- the operators together -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_draft_verify_keep_and_go_on(fmt):
+    """A prompt, a tree of drafts, the accepted path kept, the next tree: every attention against the oracle on a cache that the oracle
+    keeps by itself, and at the end all cached rows read back."""
+    import paper_2508_18850_amd as lib
+    B, nq, nkv, d, T, prompt, steps = 2, 8, 2, 64, 11, 37, 3
+    rng = np.random.default_rng(5)
+    rows = prompt + 64
+    size = 2 if fmt == "f16" else 1
+    t = {n: torch.zeros((B, nkv, rows, d * size), dtype=torch.uint8, device="cuda") for n in ("k", "v")}
+    sc = {n: torch.zeros((B, nkv, rows), device="cuda") for n in ("k", "v")}
+    cache = lib.cache_pointers(t["k"].data_ptr(), t["v"].data_ptr(), sc["k"].data_ptr(), sc["v"].data_ptr())
+    kv = lib.KvCache(nq, nkv, d, B, rows, FORMATS[fmt], 10000.0)
+    tree = lib.TreeAttention(nq, nkv, d, B, rows, FORMATS[fmt], 10000.0, T)
+    host = {n: np.zeros((B, nkv, rows, d)) for n in ("k", "v")}
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    s = _stream()
+
+    def stored(x):
+        if fmt == "f16":
+            return x.astype(np.float64)
+        code, scale = orc.encode(x, fmt)
+        return code * scale.astype(np.float64)[..., None]
+
+    def append(n, counts, depth, lens_host):
+        x = rng.standard_normal((B, n, nq + 2 * nkv, d)).astype(np.float16)
+        xd, q = _dev(x), torch.zeros((B, n, nq, d), dtype=torch.float16, device="cuda")
+        cd, dd = _dev(np.array(counts, np.int32)), _dev(depth.astype(np.int32))
+        dr = lib.draft(n, rows - n, row_len=lens.data_ptr(), row_tokens=cd.data_ptr(), depth=dd.data_ptr(), per_row=True)
+        kv.append(B, xd.data_ptr(), cache, dr, q.data_ptr(), s)
+        for b in range(B):
+            for i in range(counts[b]):
+                turned = orc.rotate(x[b, i, :nq + nkv], lens_host[b] + depth[b, i], 10000.0).astype(np.float16)
+                host["k"][b, :, lens_host[b] + i] = stored(turned[nq:])
+                host["v"][b, :, lens_host[b] + i] = stored(x[b, i, nq + nkv:])
+        torch.cuda.synchronize()
+        return q
+
+    start = [prompt, prompt - 9]
+    append(prompt, start, np.tile(np.arange(prompt), (B, 1)), [0, 0])
+    lens.copy_(_dev(np.array(start, np.int32)))
+    now = list(start)
+    for step in range(steps):
+        trees = [random_tree(rng, T) for _ in range(B)]
+        depth, mask, counts = np.stack([x[0] for x in trees]), np.stack([x[1] for x in trees]), [T, T - 3]
+        q = append(T, counts, depth, now)
+        md, dd, cd = _dev(mask_words(mask).view(np.int64)), _dev(depth), _dev(np.array(counts, np.int32))
+        out = torch.zeros((B, T, nq, d), dtype=torch.float16, device="cuda")
+        dr = lib.draft(T, rows - T, row_len=lens.data_ptr(), row_tokens=cd.data_ptr(), depth=dd.data_ptr(), tree=md.data_ptr(), per_row=True)
+        tree.attend(B, q.data_ptr(), cache, dr, 0, out.data_ptr(), s)
+        want, size_, reach = orc.attend(q.cpu().numpy(), host["k"], host["v"], now, counts, depth, mask)
+        tol = bound(want, size_, reach, d, rows)
+        got = out.cpu().numpy().astype(np.float64)
+        for b in range(B):
+            assert (np.abs(got[b, :counts[b]] - want[b, :counts[b]]) <= tol[b, :counts[b]]).all(), (step, b)
+        kept = np.zeros((B, T), np.int32)
+        n_kept = []
+        for b in range(B):                                      # a deepest path
+            leaf = int(np.argmax(depth[b, :counts[b]]))
+            path = np.nonzero(mask[b, leaf, :leaf + 1])[0]
+            kept[b, :len(path)] = path
+            n_kept.append(len(path))
+            for n in ("k", "v"):
+                host[n][b, :, now[b]:now[b] + len(path)] = host[n][b][:, now[b] + path]
+        kd, nd, new = _dev(kept), _dev(np.array(n_kept, np.int32)), torch.zeros(B, dtype=torch.int32, device="cuda")
+        kv.keep(B, cache, dr, kd.data_ptr(), nd.data_ptr(), new.data_ptr(), s)
+        lens.copy_(new)
+        now = [a + b for a, b in zip(now, n_kept)]
+        torch.cuda.synchronize()
+        assert lens.tolist() == now
+    n = min(now)
+    back = {k: torch.empty((B, nkv, n, d), dtype=torch.float16, device="cuda") for k in ("k", "v")}
+    kv.read(B, cache, 0, n, back["k"].data_ptr(), back["v"].data_ptr(), s)
+    torch.cuda.synchronize()
+    for k in ("k", "v"):
+        want = host[k][:, :, :n]
+        assert (np.abs(back[k].cpu().numpy() - want) <= 2.0 ** -11 * 1.001 * np.abs(want) + 2.0 ** -25).all()
+
+
+def test_beside_the_decode_block():
+    """One new token on the caches of the fused decode block: projection, append, attention and output projection by these calls
+    give what cf_decode_block gives in one, and the same rows in the cache."""
+    import cf_inputs
+    import paper_2508_18850_amd as lib
+    shape = cf_inputs.BlockShape("s", 512, 8, 2, 128, 10000.0, 150)
+    inp = cf_inputs.make_inputs(shape, seed=3, batch=2, kv_len=150, poison=False)
+    t = {k: torch.from_numpy(inp[k]).cuda() for k in ("x", "w_qkv", "w_o", "k_cache", "v_cache")}
+    mine = {k: t[k].clone() for k in ("k_cache", "v_cache")}
+    rows, s = inp["max_seq"], _stream()
+    out = torch.empty((2, 512), dtype=torch.float16, device="cuda")
+    block = lib.DecodeBlock(512, 8, 2, 128, 2, rows, 10000.0)
+    block.decode_block(2, t["x"].data_ptr(), t["w_qkv"].data_ptr(), t["w_o"].data_ptr(), t["k_cache"].data_ptr(), t["v_cache"].data_ptr(),
+                       150, out.data_ptr(), s)
+    block.status(s)
+    qkv = (t["x"].float() @ t["w_qkv"].float()).half()
+    q, a = (torch.empty((2, 1, 8, 128), dtype=torch.float16, device="cuda") for _ in range(2))
+    cache, draft = lib.cache_pointers(mine["k_cache"].data_ptr(), mine["v_cache"].data_ptr()), lib.draft(1, 150)
+    lib.KvCache(8, 2, 128, 2, rows, lib.CACHE_F16, 10000.0).append(2, qkv.data_ptr(), cache, draft, q.data_ptr(), s)
+    lib.TreeAttention(8, 2, 128, 2, rows, lib.CACHE_F16, 10000.0, 1).attend(2, q.data_ptr(), cache, draft, 0, a.data_ptr(), s)
+    torch.cuda.synchronize()
+    got = a.float().reshape(2, -1) @ t["w_o"].float()
+    # each of qkv, keys and attention vectors is rounded to fp16 here and not there: three times 2^-11 of the largest value or so
+    assert (got - out.float()).abs().max() <= 4 * 2.0 ** -11 * out.float().abs().max() + 2.0 ** -11 * out.float().abs().max()
+    for k in ("k_cache", "v_cache"):
+        assert torch.equal(mine[k][:, :, :150], t[k][:, :, :150])
+        d = (mine[k][:, :, 150].float() - t[k][:, :, 150].float()).abs().max()
+        assert d <= 2.0 ** -9 * t[k][:, :, 150].float().abs().max()
