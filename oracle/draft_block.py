@@ -51,13 +51,15 @@ def encode(rows, fmt):
     return code, scale.astype(np.float32)
 
 
-def attend(q, keys, values, lens, counts, depth, mask, slopes=None, cap=0.0, window=0):
+def attend(q, keys, values, lens, counts, depth, mask, slopes=None, cap=0.0, window=0,
+           value_scales=None):
     """q [B, T, nq, d], keys / values [B, nkv, rows, d] (fp64 values of the cache), lens / counts [B], depth [B, T],
     mask [B, T, T] (mask[b, t, u]: t sees the new token u).  Returns out [B, T, nq, d] (NaN for padding) and, of the same shape,
-    sum_j p_j |v_j|, and per (b, t, head) the largest sum_i |q_i k_i| / sqrt(d) of the seen keys."""
+    sum_j p_j |v_j|, per (b, t, head) the largest sum_i |q_i k_i| / sqrt(d) of the seen keys, and, of out's shape, the largest
+    p_j s_j times sum_j |v_j| / s_j, s_j the scales of the value rows ([B, nkv, rows], or 1)."""
     B, T, nq, d = q.shape
     group = nq // keys.shape[1]
-    out, size = np.full(q.shape, np.nan), np.zeros(q.shape)
+    out, size, flat = np.full(q.shape, np.nan), np.zeros(q.shape), np.zeros(q.shape)
     reach = np.zeros((B, T, nq))
     for b in range(B):
         L, n = int(lens[b]), int(counts[b])
@@ -84,4 +86,8 @@ def attend(q, keys, values, lens, counts, depth, mask, slopes=None, cap=0.0, win
                 p /= p.sum()
                 out[b, t, h] = p @ v
                 size[b, t, h] = p @ np.abs(v)
-    return out, size, reach
+                unit = np.ones(idx.size) if value_scales is None else value_scales[b, h // group, idx].astype(np.float64)
+                some = unit > 0
+                if some.any():
+                    flat[b, t, h] = (p * unit)[some].max() * (np.abs(v)[some] / unit[some, None]).sum(0)
+    return out, size, reach, flat

@@ -1,0 +1,146 @@
+// Operands of the matrix products of the tree attention (cf_tree.hip) from a key/value cache in one of its formats.
+//
+// Both products are taken transposed, so that a lane of 16 g + c has to do with one row c of queries throughout:
+//   S^T = K Q^T   16 keys x 16 queries a tile: A = keys, B = queries; the lane gets the scores of its query for keys 4 g .. 4 g + 3
+//   O^T = V^T P^T 16 dimensions x 16 queries: A = values, B = weights; the contraction runs over 32 keys in the order in which the
+//                 scores of two tiles lie in the lane (keys 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3), so that no weight moves
+// NJ = HD / 16 adjacent dimensions of a value row to a lane: dimension NJ c + jj is row c of the jj-th product.
+#ifndef CF_TREE_DEVICE_H
+#define CF_TREE_DEVICE_H
+
+#include "cf_cache_device.h"
+#include "cf_mfma_device.h"
+#include "cf_stream_device.h"
+
+namespace cf {
+namespace tree {
+
+using cf::mfma::f32x4;
+using cf::mfma::h8;
+using cf::mfma::mfma16;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+
+// fp16 pair of two codes in the low bytes of the halves.  int8 codes come with their top bit flipped (0 .. 255): such a half is the
+// fp16 number code * 2^-24, and one multiply-add makes it (code - 128) * 2^-9, exactly.
+constexpr float kInt8Unit = 512.f;          // what a code's operand has to be multiplied with
+__device__ __forceinline__ uint32_t pair_of_int8(uint32_t x)
+{
+    const h2 v = __builtin_bit_cast(h2, x) * h2{(_Float16)32768.f, (_Float16)32768.f} + h2{(_Float16)-0.25f, (_Float16)-0.25f};
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ uint32_t pair_of_e4m3(uint32_t x, bool high)
+{
+    const auto v = high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x, 1.f, false);
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// The keys of a step of 32: requested row by row, 16 bytes a load, used as A operands.
+template <int HD, int FMT>
+struct Keys {
+    static constexpr int KS = HD / 32, LOADS = FMT == CF_CACHE_F16 ? KS : KS / 2, ROW = HD * cache::kValueBytes<FMT>;
+    u32x4 raw[2][LOADS];
+    // first dimension of what group g holds for contraction step ks
+    static __device__ __forceinline__ int dim(int ks, int g) { return FMT == CF_CACHE_F16 ? 32 * ks + 8 * g : 64 * (ks / 2) + 16 * g + 8 * (ks & 1); }
+    static __device__ __forceinline__ uint32_t offset(int c, int g) { return (uint32_t)(c * ROW + 16 * g); }
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t off)
+    {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                raw[t][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + t * (16 * ROW) + 64 * i, 0, 0));
+    }
+    __device__ __forceinline__ h8 operand(int t, int ks) const
+    {
+        if constexpr (FMT == CF_CACHE_F16) {
+            return __builtin_bit_cast(h8, raw[t][ks]);
+        } else {
+            const u32x4 x = raw[t][ks / 2];
+            u32x4 o;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                uint32_t q = x[2 * (ks & 1) + w];
+                if constexpr (FMT == CF_CACHE_INT8) {
+                    q ^= 0x80808080u;
+                    o[2 * w] = pair_of_int8(__builtin_amdgcn_perm(0u, q, 0x0c010c00u));
+                    o[2 * w + 1] = pair_of_int8(__builtin_amdgcn_perm(0u, q, 0x0c030c02u));
+                } else {
+                    o[2 * w] = pair_of_e4m3(q, false);
+                    o[2 * w + 1] = pair_of_e4m3(q, true);
+                }
+            }
+            return __builtin_bit_cast(h8, o);
+        }
+    }
+};
+
+// The values of a step of 32: NJ adjacent dimensions of eight rows to a lane, transposed in the lane into NJ A operands.
+template <int HD, int FMT>
+struct Values {
+    static constexpr int NJ = HD / 16, ROW = HD * cache::kValueBytes<FMT>, DW = NJ * cache::kValueBytes<FMT> / 4;     // dwords of a load: 1, 2 or 4
+    uint32_t raw[8][DW];
+    static __device__ __forceinline__ int row(int u, int g) { return u < 4 ? 4 * g + u : 12 + 4 * g + u; }
+    static __device__ __forceinline__ uint32_t offset(int c, int g) { return (uint32_t)(4 * g * ROW + c * (4 * DW)); }
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t off)
+    {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const uint32_t at = off + (u < 4 ? u : 12 + u) * ROW;
+            if constexpr (DW == 4) {
+                const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+#pragma unroll
+                for (int w = 0; w < 4; ++w) raw[u][w] = x[w];
+            } else if constexpr (DW == 2) {
+                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0));
+                raw[u][0] = x[0], raw[u][1] = x[1];
+            } else {
+                raw[u][0] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+            }
+        }
+    }
+    __device__ __forceinline__ void operands(h8 (&f)[NJ]) const
+    {
+        u32x4 o[NJ];
+        if constexpr (FMT == CF_CACHE_F16) {
+#pragma unroll
+            for (int j2 = 0; j2 < NJ / 2; ++j2)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    o[2 * j2][w] = __builtin_amdgcn_perm(raw[2 * w + 1][j2], raw[2 * w][j2], 0x05040100u);
+                    o[2 * j2 + 1][w] = __builtin_amdgcn_perm(raw[2 * w + 1][j2], raw[2 * w][j2], 0x07060302u);
+                }
+        } else if constexpr (FMT == CF_CACHE_INT8) {
+#pragma unroll
+            for (int j4 = 0; j4 < NJ / 4; ++j4)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t lo = raw[2 * w][j4] ^ 0x80808080u, hi = raw[2 * w + 1][j4] ^ 0x80808080u;
+                    o[4 * j4][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, 0x0c040c00u));
+                    o[4 * j4 + 1][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, 0x0c050c01u));
+                    o[4 * j4 + 2][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, 0x0c060c02u));
+                    o[4 * j4 + 3][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, 0x0c070c03u));
+                }
+        } else {
+#pragma unroll
+            for (int j4 = 0; j4 < NJ / 4; ++j4)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t lo = raw[2 * w][j4], hi = raw[2 * w + 1][j4];
+                    const uint32_t a = __builtin_amdgcn_perm(hi, lo, 0x05010400u), b = __builtin_amdgcn_perm(hi, lo, 0x07030602u);
+                    o[4 * j4][w] = pair_of_e4m3(a, false);
+                    o[4 * j4 + 1][w] = pair_of_e4m3(a, true);
+                    o[4 * j4 + 2][w] = pair_of_e4m3(b, false);
+                    o[4 * j4 + 3][w] = pair_of_e4m3(b, true);
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) f[j] = __builtin_bit_cast(h8, o[j]);
+    }
+};
+
+}  // namespace tree
+}  // namespace cf
+
+#endif

@@ -48,11 +48,14 @@ def bytes_code(raw, fmt):
     return raw.view(np.int8).astype(np.float64) if fmt == "int8" else orc.E4M3[raw]
 
 
-def bound(out, size, reach, d, keys, slope_reach=0.0):
+def bound(out, size, reach, flat, d, keys, slope_reach=0.0):
     """Largest error of an element of cf_tree_attend's result.  fp16 result: 2^-11 |out|, 2^-25 near zero.  Softmax weights
     rounded to fp16 for the second product: 2^-11 of each, so 2^-11 sum p |v|, and as much again for weights that enter the
     product times a scale.  Scores in fp32: d + 8 roundings of at most sum |q k| / sqrt(d) (and of the distance bias), which moves a weight, and the sum that divides
-    it, by twice that.  Sums over the keys: one rounding per key, of both sums."""
+    it, by twice that.  Sums over the keys: one rounding per key, of both sums.
+    Weights that are small beside the row's largest: fp16 numbers below 2^-14 lie 2^-24 apart, so that a weight w_j may be off by
+    2^-25.  The largest w_j is at least 2^7 (where the reference was last moved to), w_j = p_j s_j L with s_j the scale of the value row
+    (1 in fp16) and L the row's sum, so 1 / L <= 2^-7 max(p_j s_j), and the result is off by 2^-25 sum_j |v_j / s_j| / L at most."""
     half = 2.0 ** -11
     score = 2.0 * ((d + 8) * 2.0 ** -24 * reach + 4 * 2.0 ** -24 * slope_reach)
-    return half * np.abs(out) + 2.0 ** -25 + size * (2 * half + score[..., None] + 2 * keys * 2.0 ** -24)
+    return half * np.abs(out) + 2.0 ** -25 + 2.0 ** -32 * flat + size * (2 * half + score[..., None] + 2 * keys * 2.0 ** -24)

@@ -78,17 +78,17 @@ class Case:
         return self.out.cpu().numpy()
 
     def want(self):
-        return orc.attend(self.q, self.kv, self.vv, self.lens, self.counts, self.depth, self.mask, self.slopes, self.cap, self.window)
+        return orc.attend(self.q, self.kv, self.vv, self.lens, self.counts, self.depth, self.mask, self.slopes, self.cap, self.window, self.vs)
 
     def check(self, got=None):
         got = self.run() if got is None else got
-        out, size, reach = self.want()
+        out, size, reach, flat = self.want()
         pad = np.isnan(out).all(-1)
         for b in range(self.B):
             pad[b, :self.counts[b]] = False
         assert (got[pad] == 7.0).all(), "padding was written"
         slope_reach = 0.0 if self.slopes is None else float(self.slopes.max()) * (self.max_len + self.T)
-        tol = bound(out, size, reach, self.d, max(self.lens) + self.T, slope_reach)
+        tol = bound(out, size, reach, flat, self.d, max(self.lens) + self.T, slope_reach)
         ok = np.broadcast_to(~pad[..., None], out.shape)
         # fp16 ends at 65504: from 65520 on the nearest one is infinite.  What is within its bound of that may be either.
         far = ok & (np.abs(out) - np.where(ok, tol, 0) >= 65520)
@@ -375,6 +375,7 @@ def test_draft_verify_keep_and_go_on(fmt):
     kv = lib.KvCache(nq, nkv, d, B, rows, FORMATS[fmt], 10000.0)
     tree = lib.TreeAttention(nq, nkv, d, B, rows, FORMATS[fmt], 10000.0, T)
     host = {n: np.zeros((B, nkv, rows, d)) for n in ("k", "v")}
+    unit = None if fmt == "f16" else np.zeros((B, nkv, rows))
     lens = torch.zeros(B, dtype=torch.int32, device="cuda")
     s = _stream()
 
@@ -395,6 +396,8 @@ def test_draft_verify_keep_and_go_on(fmt):
                 turned = orc.rotate(x[b, i, :nq + nkv], lens_host[b] + depth[b, i], 10000.0).astype(np.float16)
                 host["k"][b, :, lens_host[b] + i] = stored(turned[nq:])
                 host["v"][b, :, lens_host[b] + i] = stored(x[b, i, nq + nkv:])
+                if unit is not None:
+                    unit[b, :, lens_host[b] + i] = orc.encode(x[b, i, nq + nkv:], fmt)[1]
         torch.cuda.synchronize()
         return q
 
@@ -410,8 +413,8 @@ def test_draft_verify_keep_and_go_on(fmt):
         out = torch.zeros((B, T, nq, d), dtype=torch.float16, device="cuda")
         dr = lib.draft(T, rows - T, row_len=lens.data_ptr(), row_tokens=cd.data_ptr(), depth=dd.data_ptr(), tree=md.data_ptr(), per_row=True)
         tree.attend(B, q.data_ptr(), cache, dr, 0, out.data_ptr(), s)
-        want, size_, reach = orc.attend(q.cpu().numpy(), host["k"], host["v"], now, counts, depth, mask)
-        tol = bound(want, size_, reach, d, rows)
+        want, size_, reach, flat = orc.attend(q.cpu().numpy(), host["k"], host["v"], now, counts, depth, mask, value_scales=unit)
+        tol = bound(want, size_, reach, flat, d, rows)
         got = out.cpu().numpy().astype(np.float64)
         for b in range(B):
             assert (np.abs(got[b, :counts[b]] - want[b, :counts[b]]) <= tol[b, :counts[b]]).all(), (step, b)
@@ -424,6 +427,8 @@ def test_draft_verify_keep_and_go_on(fmt):
             n_kept.append(len(path))
             for n in ("k", "v"):
                 host[n][b, :, now[b]:now[b] + len(path)] = host[n][b][:, now[b] + path]
+            if unit is not None:
+                unit[b, :, now[b]:now[b] + len(path)] = unit[b][:, now[b] + path]
         kd, nd, new = _dev(kept), _dev(np.array(n_kept, np.int32)), torch.zeros(B, dtype=torch.int32, device="cuda")
         kv.keep(B, cache, dr, kd.data_ptr(), nd.data_ptr(), new.data_ptr(), s)
         lens.copy_(new)

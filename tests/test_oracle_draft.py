@@ -62,7 +62,7 @@ def test_attend_of_a_chain_is_causal_attention():
     L, T, d = 5, 4, 64
     q, k, v = rng.standard_normal((1, T, 2, d)), rng.standard_normal((1, 1, L + T, d)), rng.standard_normal((1, 1, L + T, d))
     depth, mask = random_tree(rng, T, chain=True)
-    out, _, _ = orc.attend(q, k, v, [L], [T], depth[None], mask[None])
+    out, _, _, _ = orc.attend(q, k, v, [L], [T], depth[None], mask[None])
     for t in range(T):
         s = k[0, 0, :L + t + 1] @ q[0, t, 1] / 8.0
         p = np.exp(s) / np.exp(s).sum()
@@ -73,16 +73,16 @@ def test_attend_masks_window_cap_and_empty_rows():
     rng = np.random.default_rng(3)
     q, k, v = rng.standard_normal((1, 2, 1, 64)), rng.standard_normal((1, 1, 6, 64)), rng.standard_normal((1, 1, 6, 64))
     none = np.zeros((1, 2, 2), bool)
-    out, _, _ = orc.attend(q, k, v, [0], [2], np.zeros((1, 2), np.int32), none)
+    out, _, _, _ = orc.attend(q, k, v, [0], [2], np.zeros((1, 2), np.int32), none)
     assert not out.any()                                        # sees nothing
     own = none.copy()
     own[0, 1, 1] = True
-    out, _, _ = orc.attend(q, k, v, [4], [2], np.array([[0, 1]], np.int32), own, window=1)
+    out, _, _, _ = orc.attend(q, k, v, [4], [2], np.array([[0, 1]], np.int32), own, window=1)
     assert np.allclose(out[0, 1, 0], v[0, 0, 5]) and not out[0, 0].any()
     # a bias that outweighs everything leaves the nearest key; a cap of nearly nothing leaves the mean
-    out, _, _ = orc.attend(q, k, v, [4], [2], np.array([[0, 1]], np.int32), own, slopes=[1e6])
+    out, _, _, _ = orc.attend(q, k, v, [4], [2], np.array([[0, 1]], np.int32), own, slopes=[1e6])
     assert np.allclose(out[0, 1, 0], v[0, 0, 5])
-    out, _, _ = orc.attend(q, k, v, [4], [2], np.array([[0, 1]], np.int32), own, cap=1e-9)
+    out, _, _, _ = orc.attend(q, k, v, [4], [2], np.array([[0, 1]], np.int32), own, cap=1e-9)
     assert np.allclose(out[0, 0, 0], v[0, 0, :4].mean(0))
 
 
