@@ -1,9 +1,10 @@
 // Attention of drafted tokens over a key/value cache (cf_tree_* in include/cfdecode.h).
 //
-// The rows of one KV head's queries (token t, query head hh of the group: row t * group + hh) are cut into blocks of 16 NR, the keys of a
-// sequence into parts; a workgroup takes one block over one part.  Its four wavefronts take steps of 32 keys in turn, each with all rows
-// of the block: scores and weighted values are matrix products (cf_tree_device.h), keys and values go from memory into registers as the
-// operands want them, and nothing passes through LDS until the wavefronts' results are joined.
+// The rows of one KV head's queries (token t, query head hh of the group: row t * group + hh) are cut into blocks, the keys of a sequence
+// into parts; a workgroup takes one block over one part.  Scores and weighted values are matrix products (cf_tree_device.h).  Two
+// kernels: up to 32 rows the four wavefronts of a workgroup take steps of 32 keys in turn, each with all rows, and keys and values go from
+// memory into registers as the operands want them (tree_tiles); with more rows the wavefronts divide the rows and share steps of 64 keys,
+// which are staged in LDS as fp16 (tree_blocks), so that 8-bit codes are converted once for all rows.
 //
 // Softmax in one pass.  Every row keeps a reference mm, the sum l of 2^(x_j - mm) and the sums of w_j v_j with
 // w_j = 2^(x_j - mm) * scale_j (x_j: score in units of log2 e, scale_j: scale of an 8-bit value row, else 1), so that values enter the
@@ -50,30 +51,30 @@ struct TreeArgs {
     int tree_stride, words;        // words of a batch row's masks (0: shared), of a token's mask
     int nq, nkv, group, max_seq, window;
     int splits, blocks, units;     // parts of a sequence; row blocks; batch * nkv * splits
+    int padded;                    // rows of all row blocks
     float cap;
 };
 
-__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t low_bits(int n) { return (uint32_t)(((1ull << min(max(n, 0), 32)) - 1)); }
 
-// Which of the keys j0 .. j0 + 31 token t sees: bit i for key j0 + i (without the window).
+// Which of the keys j0 .. j0 + 31 token t sees: bit i for key j0 + i (without the window).  j0 is the same in all lanes; t < 0: none.
 __device__ __forceinline__ uint32_t seen_bits(const TreeArgs &a, const uint64_t *tree, int t, int j0, int len, int n)
 {
     const int u0 = j0 - len;                                       // the new token at j0
-    uint32_t mine;
-    if (tree) {
-        const uint64_t *w = tree + (size_t)t * a.words;
-        if (u0 < 0) {
-            mine = u0 <= -32 ? 0u : (uint32_t)w[0] << -u0;
-        } else {
-            const int i = u0 >> 6, sh = u0 & 63;
-            uint64_t x = i < a.words ? w[i] >> sh : 0;
-            if (sh > 32 && i + 1 < a.words) x |= w[i + 1] << (64 - sh);
-            mine = (uint32_t)x;
-        }
-    } else {
+    uint32_t mine = 0;
+    if (!tree) {
         mine = low_bits(t - u0 + 1);
+    } else if (u0 > -32) {
+        const uint64_t *w = tree + (size_t)max(t, 0) * a.words;
+        const int i = max(u0, 0) >> 6, sh = max(u0, 0) & 63;
+        if (i < a.words) {
+            uint64_t x = w[i] >> sh;
+            if (sh > 32 && i + 1 < a.words) x |= w[i + 1] << (64 - sh);
+            mine = (uint32_t)x << max(-u0, 0);
+        }
     }
-    return (low_bits(len - j0) | (mine & ~low_bits(-u0))) & low_bits(len + n - j0);
+    const uint32_t seen = (low_bits(len - j0) | (mine & ~low_bits(-u0))) & low_bits(len + n - j0);
+    return t < 0 ? 0u : seen;
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -84,78 +85,251 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
 
-template <int HD, int NR>
-constexpr int kWaveFloats = 16 * (HD + 4) > NR * 16 * kStep ? 16 * (HD + 4) : NR * 16 * kStep;
+constexpr int kFar = 0x3fffffff;
+
+// In the kernels below no branch inside the loops over the keys depends on the lane: conditions of lanes are selections, and addresses of
+// lanes without a value are taken to one that is there.  (The register allocator of this compiler, when it runs out of registers, has put
+// copies for all lanes into the end of a branch that only some lanes take, and the others then had stale values.)
+
+// What a workgroup knows of its batch row.
+struct Sequence {
+    int n, len, end;               // new tokens, cached rows, their sum
+    const int32_t *depth;
+    const uint64_t *tree;
+    __device__ __forceinline__ Sequence(const TreeArgs &a, int b)
+        : n(__builtin_amdgcn_readfirstlane(a.rows.fresh(b))), len(__builtin_amdgcn_readfirstlane(a.rows.cached(b))), end(len + n), depth(a.depth ? a.depth + (size_t)b * a.depth_stride : nullptr),
+          tree(a.tree ? a.tree + (size_t)b * a.tree_stride : nullptr)
+    {
+    }
+    // of new token u (taken into 0 .. n - 1); kept where differences do not overflow
+    __device__ __forceinline__ int position(int u) const
+    {
+        u = min(max(u, 0), n - 1);
+        const int p = __builtin_elementwise_add_sat(len, depth ? depth[u] : u);
+        return min(max(p, -kFar), kFar);
+    }
+};
+
+// One row of queries of a lane.
+struct Row {
+    int tok;                       // its token, -1: padding
+    int at;                        // position and slope (times log2 e): with FORMS
+    float slope;
+};
+
+// Scores as they come out of the product: factors to units of log2 e (without a cap), and the forms of the score.
+template <int HD, int FMT>
+__device__ __forceinline__ float score_factor(float cap)
+{
+    const float unit = (FMT == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f) * (HD == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
+    return cap > 0.f ? unit * 2.f / cap : unit;                    // with a cap: twice its share of the cap, for the tanh
+}
+
+// The weights of a row for TILES tiles of 16 keys from j0 on, as B operands of the second product; moves the row's reference where
+// they ask for it.  MASKED: some row of the workgroup does not see all of these keys.
+template <int HD, int FMT, bool FORMS, bool MASKED, int TILES>
+__device__ __forceinline__ void weights(const TreeArgs &a, const Sequence &sq, const Row &row, int g, int j0, float to_score, const f32x4 (&s)[TILES],
+                                        const f32x4 (&kscale)[TILES], const f32x4 (&vscale)[TILES], float &mm, float &l, f32x4 (&acc)[HD / 16], h8 (&w)[TILES / 2])
+{
+    constexpr bool SCALED = FMT != CF_CACHE_F16;
+    constexpr int N = 4 * TILES;
+    float x[N], p[N], wt[N];
+    if constexpr (FORMS || MASKED) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int i = 16 * (e >> 2) + 4 * g + (e & 3), j = j0 + i;
+            if (MASKED && e % 8 == 0) bits = seen_bits(a, sq.tree, row.tok, j0 + 4 * e, sq.len, sq.n);
+            x[e] = s[e >> 2][e & 3] * (SCALED ? kscale[e >> 2][e & 3] : to_score);
+            bool seen = !MASKED || (bits >> (i & 31) & 1);
+            if constexpr (FORMS) {
+                int key_at = j;
+                if (MASKED) {
+                    const int new_at = sq.position(j - sq.len);
+                    key_at = j >= sq.len ? new_at : j;
+                }
+                const int distance = row.at - key_at;
+                if (a.cap > 0.f) x[e] = a.cap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(exp2_(x[e]) + 1.f));      // tanh
+                x[e] -= row.slope * (float)distance;
+                if (MASKED && a.window > 0) seen = seen && distance < a.window;
+            }
+            if (!seen) x[e] = -INFINITY;
+        }
+    }
+    auto weigh = [&]() {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if constexpr (FORMS || MASKED)
+                p[e] = exp2_(x[e] - mm);
+            else
+                p[e] = exp2_(fmaf(s[e >> 2][e & 3], SCALED ? kscale[e >> 2][e & 3] : to_score, -mm));
+            wt[e] = SCALED ? p[e] * vscale[e >> 2][e & 3] : p[e];
+            if (SCALED && MASKED && x[e] == -INFINITY) wt[e] = 0.f;         // (the scale of an unseen row may be anything)
+        }
+    };
+    weigh();
+    float most = fmaxf(wt[0], wt[1]);
+#pragma unroll
+    for (int e = 2; e < N; e += 2) most = fmaxf(fmaxf(most, wt[e]), wt[e + 1]);
+    if (__any(most > kMostWeight)) {
+        float top = kNone;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            float y = FORMS || MASKED ? x[e] : s[e >> 2][e & 3] * (SCALED ? kscale[e >> 2][e & 3] : to_score);
+            if (SCALED) y += __builtin_amdgcn_logf(vscale[e >> 2][e & 3]);
+            top = fmaxf(top, MASKED && x[e] == -INFINITY ? kNone : y);
+        }
+        top = cf::lanes::max_groups<16>(top);
+        most = cf::lanes::max_groups<16>(most);
+        const float to = most > kMostWeight ? top - kTopExponent : mm, by = exp2_(mm - to);
+        mm = to;
+        l *= by;
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j) acc[j] *= by;
+        weigh();
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; e += 4) sum += (p[e] + p[e + 1]) + (p[e + 2] + p[e + 3]);
+    l += sum;
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e >> 3][e & 7] = (_Float16)wt[e];
+}
+
+// Value rows with infinities or NaN that some row does not see would enter its product as 0 times that.  Where a step holds one, such
+// values are left out of the product, and this adds them, key by key, to the rows that see them.  dim(j, rr): dimension of acc[j][rr].
+template <int HD, int FMT, int TILES, typename Dim>
+__device__ __forceinline__ void add_unfit(__amdgpu_buffer_rsrc_t vr, int j0, int c, const h8 (&w)[TILES / 2], f32x4 (&acc)[HD / 16], Dim dim)
+{
+    constexpr int ROW = HD * kValueBytes<FMT>;
+#pragma unroll 1
+    for (int i = 0; i < 16 * TILES; ++i) {
+        const int element = 4 * (i >> 4) + (i & 3);                 // key i is this element of lane group (i / 4) % 4
+        float wt = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4 * TILES; ++e) wt = e == element ? (float)w[e >> 3][e & 7] : wt;
+        wt = __shfl(wt, 16 * ((i >> 2) & 3) + c);
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j)
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr) {
+                const uint32_t at = (uint32_t)(j0 + i) * ROW + dim(j, rr) * kValueBytes<FMT>;
+                float x;
+                if constexpr (FMT == CF_CACHE_F16) {
+                    x = (float)__builtin_bit_cast(_Float16, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(vr, at, 0, 0));
+                } else {
+                    float f[4];
+                    decode4<FMT>((uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(vr, at, 0, 0), f);
+                    x = f[0];
+                }
+                acc[j][rr] += (!(fabsf(x) <= 65504.f) && wt != 0.f) ? wt * x : 0.f;
+            }
+    }
+}
+__device__ __forceinline__ uint32_t unfit_bits(uint32_t pair) { return ((pair & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t without_unfit(uint32_t pair)
+{
+    const uint32_t bad = unfit_bits(pair);
+    return pair & ~((bad >> 15) * 0xffffu);
+}
+
+// Keys of a part in steps of STEP, counted from key 0, and from which key on all rows of the workgroup see all cached rows.
+template <bool FORMS, int STEP>
+struct Part {
+    int begin, end, all_from;
+    __device__ __forceinline__ Part(const TreeArgs &a, const Sequence &sq, int split, int nearest, int farthest)
+    {
+        int lo = 0;
+        all_from = 0;
+        if (FORMS && a.window > 0) {
+            lo = min(max(nearest - a.window + 1, 0), sq.len);
+            all_from = max(farthest - a.window + 1, 0);
+        }
+        const int first = lo / STEP, steps = (sq.end + STEP - 1) / STEP - first, per = (steps + a.splits - 1) / a.splits;
+        begin = first + split * per, end = min(first + steps, begin + per);
+    }
+};
+
+// Where a workgroup works: workgroup i runs on die i mod 8, and the row blocks of a unit (a sequence's head and part), which read the same
+// keys and values, follow each other on one die.
+struct Place {
+    int unit, block, bh, split, b, head;
+    __device__ __forceinline__ explicit Place(const TreeArgs &a)
+    {
+        const int turn = blockIdx.x >> 3;
+        unit = turn / a.blocks * 8 + (blockIdx.x & 7), block = turn % a.blocks;
+        bh = unit / a.splits, split = unit - bh * a.splits;
+        b = bh / a.nkv, head = bh - b * a.nkv;
+    }
+    __device__ __forceinline__ Place(const TreeArgs &a, int bh) : unit(0), block(0), bh(bh), split(0), b(bh / a.nkv), head(bh % a.nkv) {}
+};
+
+// Queries of a row as B operands (dims(ks): first dimension of this lane's eight in contraction step ks) and what else a row has.
+template <int HD, bool FORMS, typename Dims>
+__device__ __forceinline__ Row load_row(const TreeArgs &a, const Sequence &sq, const Place &at, int index, h8 (&q)[HD / 32], int &nearest, int &farthest, Dims dims)
+{
+    const bool there = index / a.group < sq.n;
+    const int from = min(index, sq.n * a.group - 1), t = from / a.group, hh = from - t * a.group;
+    Row row = {there ? t : -1, 0, 0.f};
+    const uint16_t *src = a.q + (((size_t)at.b * a.rows.tokens + t) * a.nq + at.head * a.group + hh) * HD;
+#pragma unroll
+    for (int ks = 0; ks < HD / 32; ++ks) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(src + dims(ks));
+        q[ks] = __builtin_bit_cast(h8, there ? x : u32x4{0u, 0u, 0u, 0u});
+    }
+    if constexpr (FORMS) {
+        row.at = sq.position(t);
+        row.slope = a.slopes ? a.slopes[at.head * a.group + hh] * kLog2e : 0.f;
+        nearest = min(nearest, row.at), farthest = max(farthest, row.at);      // (a row of padding repeats the last one)
+    }
+    return row;
+}
+__device__ __forceinline__ uint16_t *out_row(const TreeArgs &a, const Place &at, int index, int hd)
+{
+    const int t = index / a.group, hh = index - t * a.group;
+    return a.out + (((size_t)at.b * a.rows.tokens + t) * a.nq + at.head * a.group + hh) * hd;
+}
+template <int FMT>
+constexpr float kValueUnit = FMT == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f;
 
 // FORMS: the scores may be capped, biased or windowed.
 template <int HD, int FMT, int NR, bool FORMS>
-__global__ __launch_bounds__(NT, NR == 4 ? 1 : 2) void tree_tiles(const TreeArgs a)
+__global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
 {
     constexpr int KS = HD / 32, NJ = HD / 16, ROW = HD * kValueBytes<FMT>;
     constexpr bool SCALED = FMT != CF_CACHE_F16;
-    __shared__ float smem[NW * kWaveFloats<HD, NR>];
+    __shared__ float smem[NW * 16 * (HD + 4)];
     __shared__ float2 ml[NW][16 * NR];
     __shared__ float scales[NW][2][kStep];
-    const int tid = threadIdx.x, wv = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
-    // Workgroup i runs on die i mod 8: the row blocks of a unit, which read the same keys and values, follow each other on one die.
-    const int turn = blockIdx.x >> 3, unit = turn / a.blocks * 8 + (blockIdx.x & 7), block = turn % a.blocks;
-    if (unit >= a.units) return;
-    const int bh = unit / a.splits, split = unit - bh * a.splits, b = bh / a.nkv, head = bh - b * a.nkv;
-    const int n = a.rows.fresh(b), len = a.rows.cached(b), end = len + n;
-    const int first_row = block * (16 * NR), live = min(n * a.group - first_row, 16 * NR);
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const Place place(a);
+    if (place.unit >= a.units) return;
+    const Sequence sq(a, place.b);
+    const int first_row = place.block * (16 * NR), live = min(sq.n * a.group - first_row, 16 * NR);
     if (live <= 0) return;
-    const int32_t *depth = a.depth ? a.depth + (size_t)b * a.depth_stride : nullptr;
-    const uint64_t *tree = a.tree ? a.tree + (size_t)b * a.tree_stride : nullptr;
 
-    // ---- the rows of this lane: queries as B operands, positions
     h8 q[NR][KS];
-    int tok[NR];
-    [[maybe_unused]] int at[NR];
-    [[maybe_unused]] float slope[NR];
-    int nearest = 0x3fffffff, farthest = -0x3fffffff;               // of the positions of the block's tokens
+    Row row[NR];
+    int nearest = kFar, farthest = -kFar;                           // of the positions of the block's tokens
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const int row = first_row + 16 * r + c, t = row / a.group, hh = row - t * a.group;
-        tok[r] = t < n ? t : -1;
-        if (t < n) {
-            const uint16_t *src = a.q + (((size_t)b * a.rows.tokens + t) * a.nq + head * a.group + hh) * HD;
+    for (int r = 0; r < NR; ++r)
+        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + 16 * r + c, q[r], nearest, farthest, [&](int ks) { return Keys<HD, FMT>::dim(ks, g); });
+    if (FORMS && a.window > 0)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[r][ks] = *reinterpret_cast<const h8 *>(src + Keys<HD, FMT>::dim(ks, g));
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[r][ks] = h8{};
-        }
-        if constexpr (FORMS) {
-            at[r] = 0, slope[r] = 0.f;
-            if (t < n) {
-                const long long p = (long long)len + (depth ? depth[t] : t);
-                at[r] = (int)min(max(p, -0x3fffffffLL), 0x3fffffffLL);
-                nearest = min(nearest, at[r]), farthest = max(farthest, at[r]);
-                slope[r] = a.slopes ? a.slopes[head * a.group + hh] * kLog2e : 0.f;
-            }
-        }
-    }
+        for (int s = 1; s < 16; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
+    const Part<FORMS, kStep> part(a, sq, place.split, nearest, farthest);
 
-    // ---- the keys of this part: steps of 32, counted from key 0
-    int lo = 0, all_from = 0;                                       // the first key that some row sees, that all rows see
-    if constexpr (FORMS) {
-        if (a.window > 0) {
-#pragma unroll
-            for (int s = 1; s < 64; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
-            lo = min(max(nearest - a.window + 1, 0), len);
-            all_from = max(farthest - a.window + 1, 0);
-        }
-    }
-    const int step0 = lo / kStep, steps = (end + kStep - 1) / kStep - step0, per = (steps + a.splits - 1) / a.splits;
-    const int s_begin = step0 + split * per, s_end = min(step0 + steps, s_begin + per);
-
-    const size_t slice = (size_t)bh * a.max_seq;
-    const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)end * ROW);
+    const size_t slice = (size_t)place.bh * a.max_seq;
+    const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
     const float *scale_src = SCALED ? (lane < 32 ? a.k_scale : a.v_scale) + slice : nullptr;
-    const float unit_k = (FMT == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f) * (HD == 64 ? 0.125f : 0.08838834764831845f);
-    // what a score is multiplied with: to units of log2 e, or, with a cap, to twice its share of the cap in the same units
-    const float to_score = FORMS && a.cap > 0.f ? unit_k * 2.f * kLog2e / a.cap : unit_k * kLog2e;
+    const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
 
     Keys<HD, FMT> keys;
     Values<HD, FMT> vals;
@@ -170,18 +344,18 @@ __global__ __launch_bounds__(NT, NR == 4 ? 1 : 2) void tree_tiles(const TreeArgs
     }
     const uint32_t koff = Keys<HD, FMT>::offset(c, g), voff = Values<HD, FMT>::offset(c, g);
     auto load_scale = [&](int step) {
-        if constexpr (SCALED) scale = scale_src[min(step * kStep + (lane & 31), end - 1)];
+        if constexpr (SCALED) scale = scale_src[min(step * kStep + (lane & 31), sq.end - 1)];
     };
-    int step = s_begin + wv;
-    if (step < s_end) {
+    int step = part.begin + wv;
+    if (step < part.end) {
         load_scale(step);
         keys.load(kr, koff + (uint32_t)step * (kStep * ROW));
         vals.load(vr, voff + (uint32_t)step * (kStep * ROW));
     }
-    for (; step < s_end; step += NW) {
+    for (; step < part.end; step += NW) {
         const int j0 = step * kStep;
-        const bool masked = j0 + kStep > len || j0 < all_from;      // (the same for the whole wavefront)
-        const uint32_t next = (uint32_t)min(step + NW, s_end - 1) * (kStep * ROW);
+        const bool masked = j0 + kStep > sq.len || j0 < part.all_from;      // (the same for the whole wavefront)
+        const int next = min(step + NW, part.end - 1);
         if constexpr (SCALED) {
             const float x = lane < 32 ? scale * to_score : fabsf(scale) < kSmallScale ? kSmallScale : scale;
             scales[wv][lane >> 5][lane & 31] = x;
@@ -196,7 +370,7 @@ __global__ __launch_bounds__(NT, NR == 4 ? 1 : 2) void tree_tiles(const TreeArgs
 #pragma unroll
                 for (int r = 0; r < NR; ++r) s[r][t] = mfma16(k, q[r][ks], ks ? s[r][t] : f32x4{0.f, 0.f, 0.f, 0.f});
             }
-        keys.load(kr, koff + next);
+        keys.load(kr, koff + (uint32_t)next * (kStep * ROW));
         f32x4 kscale[2], vscale[2];
         if constexpr (SCALED) {
             wave_sync();
@@ -206,117 +380,43 @@ __global__ __launch_bounds__(NT, NR == 4 ? 1 : 2) void tree_tiles(const TreeArgs
                 vscale[t] = *reinterpret_cast<const f32x4 *>(&scales[wv][1][16 * t + 4 * g]);
             }
             wave_sync();
-            load_scale(min(step + NW, s_end - 1));
+            load_scale(next);
         }
         // ---- weights
-        h8 w[NR];
+        h8 w[NR][1];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            float x[8], p[8], wt[8];
-            if (FORMS || masked) {
-                const uint32_t bits = !masked ? ~0u : tok[r] < 0 ? 0u : seen_bits(a, tree, tok[r], j0, len, n);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int i = 16 * (e >> 2) + 4 * g + (e & 3), j = j0 + i;
-                    x[e] = s[r][e >> 2][e & 3] * (SCALED ? kscale[e >> 2][e & 3] : to_score);
-                    bool seen = bits >> i & 1;
-                    if constexpr (FORMS) {
-                        int key_at = j;
-                        if (masked && j >= len && depth) key_at = j < end ? (int)min(max((long long)len + depth[j - len], -0x3fffffffLL), 0x3fffffffLL) : 0;
-                        const int distance = at[r] - key_at;
-                        if (a.cap > 0.f) x[e] = a.cap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(exp2_(x[e]) + 1.f));      // tanh
-                        x[e] -= slope[r] * (float)distance;
-                        if (masked && a.window > 0) seen = seen && distance < a.window;
-                    }
-                    if (masked && !seen) x[e] = -INFINITY;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = s[r][e >> 2][e & 3] * (SCALED ? kscale[e >> 2][e & 3] : to_score);
-            }
-            auto weigh = [&]() {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    p[e] = exp2_(x[e] - mm[r]);
-                    wt[e] = SCALED ? p[e] * vscale[e >> 2][e & 3] : p[e];
-                    if (SCALED && masked && x[e] == -INFINITY) wt[e] = 0.f;             // (the scale of an unseen row may be anything)
-                }
-            };
-            weigh();
-            float most = fmaxf(fmaxf(fmaxf(wt[0], wt[1]), fmaxf(wt[2], wt[3])), fmaxf(fmaxf(wt[4], wt[5]), fmaxf(wt[6], wt[7])));
-            if (__any(most > kMostWeight)) {
-                float top = kNone;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float y = SCALED ? x[e] + __builtin_amdgcn_logf(vscale[e >> 2][e & 3]) : x[e];
-                    top = fmaxf(top, masked && x[e] == -INFINITY ? kNone : y);
-                }
-                top = cf::lanes::max_groups<16>(top);
-                most = cf::lanes::max_groups<16>(most);
-                const float to = most > kMostWeight ? top - kTopExponent : mm[r], by = exp2_(mm[r] - to);
-                mm[r] = to;
-                l[r] *= by;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[r][j] *= by;
-                weigh();
-            }
-            l[r] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[r][e] = (_Float16)wt[e];
+            if (masked)
+                weights<HD, FMT, FORMS, true, 2>(a, sq, row[r], g, j0, to_score, s[r], kscale, vscale, mm[r], l[r], acc[r], w[r]);
+            else
+                weights<HD, FMT, FORMS, false, 2>(a, sq, row[r], g, j0, to_score, s[r], kscale, vscale, mm[r], l[r], acc[r], w[r]);
         }
         // ---- values
         h8 v[NJ];
         vals.operands(v);
         if (FMT != CF_CACHE_INT8 && masked) {
-            // 0 times an infinity or a NaN of an unseen value row would be NaN: where the step holds one, such values are left out of the
-            // product and added, token by token, to the rows that see them.
             uint32_t odd = 0;
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) odd |= (__builtin_bit_cast(cf::tree::u32x4, v[j])[d] & 0x7c007c00u) + 0x04000400u;
-            if (__any(odd & 0x80008000u)) {
+                for (int d = 0; d < 4; ++d) odd |= unfit_bits(__builtin_bit_cast(cf::tree::u32x4, v[j])[d]);
+            if (__any(odd)) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
+                for (int j = 0; j < NJ; ++j) {
+                    cf::tree::u32x4 x = __builtin_bit_cast(cf::tree::u32x4, v[j]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if ((__builtin_bit_cast(uint16_t, (_Float16)v[j][e]) & 0x7c00u) == 0x7c00u) v[j][e] = (_Float16)0.f;
-                float *tmp = smem + wv * kWaveFloats<HD, NR>;                          // [r][key][row]
-                wave_sync();
+                    for (int d = 0; d < 4; ++d) x[d] = without_unfit(x[d]);
+                    v[j] = __builtin_bit_cast(h8, x);
+                }
 #pragma unroll
-                for (int r = 0; r < NR; ++r)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) tmp[(r * kStep + 16 * (e >> 2) + 4 * g + (e & 3)) * 16 + c] = (float)w[r][e];
-                wave_sync();
-#pragma unroll 1
-                for (int i = 0; i < kStep; ++i)
-#pragma unroll
-                    for (int rr = 0; rr < 4; ++rr)
-#pragma unroll
-                        for (int j = 0; j < NJ; ++j) {
-                            const uint32_t d = (uint32_t)(j0 + i) * ROW + (NJ * (4 * g + rr) + j) * kValueBytes<FMT>;
-                            float x;
-                            if constexpr (FMT == CF_CACHE_F16) {
-                                x = (float)__builtin_bit_cast(_Float16, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(vr, d, 0, 0));
-                            } else {
-                                float f[4];
-                                decode4<FMT>((uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(vr, d, 0, 0), f);
-                                x = f[0];
-                            }
-                            if (!(fabsf(x) <= 65504.f))
-#pragma unroll
-                                for (int r = 0; r < NR; ++r) {
-                                    const float wt = tmp[(r * kStep + i) * 16 + c];
-                                    if (wt != 0.f) acc[r][j][rr] += wt * x;
-                                }
-                        }
+                for (int r = 0; r < NR; ++r) add_unfit<HD, FMT, 2>(vr, j0, c, w[r], acc[r], [&](int j, int rr) { return NJ * (4 * g + rr) + j; });
             }
         }
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int r = 0; r < NR; ++r) acc[r][j] = mfma16(v[j], w[r], acc[r][j]);
-        vals.load(vr, voff + next);
+            for (int r = 0; r < NR; ++r) acc[r][j] = mfma16(v[j], w[r][0], acc[r][j]);
+        vals.load(vr, voff + (uint32_t)next * (kStep * ROW));
     }
 
     // ---- the wavefronts' results joined, 16 rows at a time
@@ -337,92 +437,315 @@ __global__ __launch_bounds__(NT, NR == 4 ? 1 : 2) void tree_tiles(const TreeArgs
                 *reinterpret_cast<float4 *>(smem + (wv * 16 + c) * (HD + 4) + NJ * (4 * g + rr) + j) =
                     make_float4(acc[r][j][rr], acc[r][j + 1][rr], acc[r][j + 2][rr], acc[r][j + 3][rr]);
         __syncthreads();
-        const int row = 16 * r + row16;
-        if (row16 < 16 && row < live) {
+        const int i = 16 * r + row16;
+        if (row16 < 16 && i < live) {
             float m = kNone, total = 0.f, o[8] = {};
 #pragma unroll
-            for (int k = 0; k < NW; ++k) m = fmaxf(m, ml[k][row].x);
+            for (int k = 0; k < NW; ++k) m = fmaxf(m, ml[k][i].x);
 #pragma unroll
             for (int k = 0; k < NW; ++k) {
-                const float f = exp2_(ml[k][row].x - m);
+                const float f = exp2_(ml[k][i].x - m);
                 const float *src = smem + (k * 16 + row16) * (HD + 4) + d0;
-                total += f * ml[k][row].y;
+                total += f * ml[k][i].y;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] += f * src[e];
             }
             if (a.splits > 1) {
-                const size_t at_row = (size_t)unit * (a.blocks * 16 * NR) + first_row + row;
-                float4 *dst = reinterpret_cast<float4 *>(a.part + at_row * HD + d0);
+                const size_t at = (size_t)place.unit * a.padded + first_row + i;
+                float4 *dst = reinterpret_cast<float4 *>(a.part + at * HD + d0);
                 dst[0] = make_float4(o[0], o[1], o[2], o[3]);
                 dst[1] = make_float4(o[4], o[5], o[6], o[7]);
-                if (d0 == 0) a.part_ml[at_row] = make_float2(m, total);
+                if (d0 == 0) a.part_ml[at] = make_float2(m, total);
             } else {
-                const int t = (first_row + row) / a.group, hh = first_row + row - t * a.group;
-                const float inv = total == 0.f ? 0.f : (FMT == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f) / total;
+                const float inv = total == 0.f ? 0.f : kValueUnit<FMT> / total;
                 h8 res;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) res[e] = (_Float16)(o[e] * inv);
-                *reinterpret_cast<h8 *>(a.out + (((size_t)b * a.rows.tokens + t) * a.nq + head * a.group + hh) * HD + d0) = res;
+                *reinterpret_cast<h8 *>(out_row(a, place, first_row + i, HD) + d0) = res;
             }
         }
     }
 }
 
-// The parts of a sequence joined, in their order: eight dimensions of a row to a thread.
+// Staged steps: 64 rows of keys and of values as fp16 in LDS, two steps deep.  A row of keys is 16 bytes longer than its values, so that the
+// sixteen rows of an operand start in different banks; a row of values 32 bytes, for the transposing reads of four rows by 16 dimensions.
+constexpr int kBlockStep = 64;
 template <int HD>
-__global__ __launch_bounds__(NT) void tree_join(const TreeArgs a, int padded, float unit_v)
+struct Stage {
+    static constexpr int KROW = 2 * HD + 16, VROW = 2 * HD + 32;
+    char k[2][kBlockStep * KROW], v[2][kBlockStep * VROW];
+    float scale[2][2][kBlockStep];
+    int unfit[2];                  // 1 + the step of this buffer that holds infinities or NaN among its values
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+// A operand of 16 dimensions from dim on and the keys of one h8 of weights: of keys first + 4 g .. + 3 and first + 16 + 4 g .. + 3.
+template <int VROW>
+__device__ __forceinline__ h8 transposed(const char *v, int first, int dim, int c, int g)
 {
-    constexpr int CH = HD / 8;
-    const int bh = blockIdx.y, b = bh / a.nkv, head = bh - b * a.nkv;
-    const int row = blockIdx.x * (NT / CH) + threadIdx.x / CH, d0 = 8 * (threadIdx.x % CH);
+    using Ptr = __attribute__((address_space(3))) s16x4 *;
+    const char *at = v + (first + 4 * g + (c >> 2)) * VROW + 2 * (dim + 4 * (c & 3));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(at + 16 * VROW));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(h8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// WV wavefronts with 16 NR rows each share the steps of a part.
+template <int HD, int FMT, int WV, int NR, bool FORMS>
+__global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
+{
+    constexpr int KS = HD / 32, NJ = HD / 16, ROW = HD * kValueBytes<FMT>, T = 64 * WV;
+    constexpr bool SCALED = FMT != CF_CACHE_F16;
+    // 16-byte pieces of a row; of the keys of a step, to a thread.  Where there are more threads than pieces the first ones have the keys,
+    // the last ones the values.
+    constexpr int PPR = ROW / 16, ALL = kBlockStep * PPR, PIECES = ALL < T ? 1 : ALL / T, APART = ALL < T ? T - ALL : 0;
+    static_assert(ALL % T == 0 || 2 * ALL == T, "every thread stages as much");
+    using S = Stage<HD>;
+    __shared__ S lds;
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const Place place(a);
+    if (place.unit >= a.units) return;
+    const Sequence sq(a, place.b);
+    const int first_row = place.block * (16 * NR * WV), live = min(sq.n * a.group - first_row, 16 * NR * WV);
+    if (live <= 0) return;
+    const int my_rows = 16 * NR * wv;                               // first of this wavefront's rows in the block
+
+    h8 q[NR][KS];
+    Row row[NR];
+    int nearest = kFar, farthest = -kFar;
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + my_rows + 16 * r + c, q[r], nearest, farthest, [&](int ks) { return 32 * ks + 8 * g; });
+    if (FORMS && a.window > 0) {                                    // the part is the whole block's: its extremes by way of LDS
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
+        int *ends = reinterpret_cast<int *>(lds.k[0]);
+        if (lane == 0) ends[2 * wv] = nearest, ends[2 * wv + 1] = farthest;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WV; ++i) nearest = min(nearest, ends[2 * i]), farthest = max(farthest, ends[2 * i + 1]);
+        __syncthreads();
+    }
+    const Part<FORMS, kBlockStep> part(a, sq, place.split, nearest, farthest);
+
+    const size_t slice = (size_t)place.bh * a.max_seq;
+    const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
+    const float *scale_src = SCALED ? (wv == 1 ? a.v_scale : a.k_scale) + slice : nullptr;
+    const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
+
+    f32x4 acc[NR][NJ];
+    float mm[NR], l[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        mm[r] = kNone, l[r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // ---- staging: requested a step ahead of the one that is written, which is a step ahead of the one that is used
+    u32x4 kraw[PIECES], vraw[PIECES];
+    float scale = 0.f;
+    auto request = [&](int step) {
+        const uint32_t off = (uint32_t)step * (kBlockStep * ROW) + 16 * tid;
+        if (!APART || 64 * wv < ALL)
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) kraw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, off + 16 * T * i, 0, 0));
+        if (!APART || 64 * wv >= APART)
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) vraw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, off + 16 * (T * i - APART), 0, 0));
+        if (SCALED && wv < 2) scale = scale_src[min(step * kBlockStep + lane, sq.end - 1)];
+    };
+    auto masked_step = [&](int step) { return (step + 1) * kBlockStep > sq.len || step * kBlockStep < part.all_from; };
+    auto write = [&](int step) {
+        const int buf = (step - part.begin) & 1;
+        const bool look = FMT != CF_CACHE_INT8 && masked_step(step);
+        uint32_t odd = 0;
+        auto put = [&](char *rows, int row_bytes, const u32x4 &raw, int piece, bool check) {
+            char *dst = rows + piece / PPR * row_bytes + piece % PPR * (FMT == CF_CACHE_F16 ? 16 : 32);
+#pragma unroll
+            for (int half = 0; half < (FMT == CF_CACHE_F16 ? 1 : 2); ++half) {
+                u32x4 x = raw;
+                if constexpr (FMT != CF_CACHE_F16) x = cf::tree::widen<FMT>(raw[2 * half], raw[2 * half + 1]);
+                if (check)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) odd |= unfit_bits(x[d]), x[d] = without_unfit(x[d]);
+                *reinterpret_cast<u32x4 *>(dst + 16 * half) = x;
+            }
+        };
+        if (!APART || 64 * wv < ALL)
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) put(lds.k[buf], S::KROW, kraw[i], tid + T * i, false);
+        if (!APART || 64 * wv >= APART)
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) put(lds.v[buf], S::VROW, vraw[i], tid + T * i - APART, look);
+        if (look && __any(odd)) lds.unfit[buf] = 1 + step;
+        if (SCALED && wv < 2)
+            lds.scale[buf][wv][lane] = wv == 0 ? scale * to_score : fabsf(scale) < kSmallScale ? kSmallScale : scale;
+    };
+    if (tid < 2) lds.unfit[tid] = 0;
+    __syncthreads();
+    if (part.begin < part.end) {
+        request(part.begin);
+        write(part.begin);
+        request(min(part.begin + 1, part.end - 1));
+    }
+    for (int step = part.begin; step < part.end; ++step) {
+        lds_barrier();                                              // this step is written, and the other buffer has been read
+        if (step + 1 < part.end) {
+            write(step + 1);
+            request(min(step + 2, part.end - 1));
+        }
+        if (my_rows >= live) continue;                              // a wavefront without rows only stages
+        const int buf = (step - part.begin) & 1, j0 = step * kBlockStep;
+        const char *kb = lds.k[buf], *vb = lds.v[buf];
+        f32x4 s[NR][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const h8 k = *reinterpret_cast<const h8 *>(kb + (16 * t + c) * S::KROW + 64 * ks + 16 * g);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) s[r][t] = mfma16(k, q[r][ks], ks ? s[r][t] : f32x4{0.f, 0.f, 0.f, 0.f});
+            }
+        f32x4 kscale[4], vscale[4];
+        if constexpr (SCALED) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                kscale[t] = *reinterpret_cast<const f32x4 *>(&lds.scale[buf][0][16 * t + 4 * g]);
+                vscale[t] = *reinterpret_cast<const f32x4 *>(&lds.scale[buf][1][16 * t + 4 * g]);
+            }
+        }
+        h8 w[NR][2];
+        const bool masked = masked_step(step);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            if (masked)
+                weights<HD, FMT, FORMS, true, 4>(a, sq, row[r], g, j0, to_score, s[r], kscale, vscale, mm[r], l[r], acc[r], w[r]);
+            else
+                weights<HD, FMT, FORMS, false, 4>(a, sq, row[r], g, j0, to_score, s[r], kscale, vscale, mm[r], l[r], acc[r], w[r]);
+        }
+        if (FMT != CF_CACHE_INT8 && masked && __builtin_amdgcn_readfirstlane(lds.unfit[buf]) == 1 + step)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) add_unfit<HD, FMT, 4>(vr, j0, c, w[r], acc[r], [&](int j, int rr) { return 16 * j + 4 * g + rr; });
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const h8 v = transposed<S::VROW>(vb, 32 * half, 16 * j, c, g);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) acc[r][j] = mfma16(v, w[r][half], acc[r][j]);
+            }
+    }
+
+#pragma unroll
+    for (int r = 0; r < NR; ++r) l[r] = cf::lanes::sum_groups<16>(l[r]);
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int i = my_rows + 16 * r + c;
+        const float total = l[r];
+        if (i < live && a.splits > 1) {
+            const size_t at = (size_t)place.unit * a.padded + first_row + i;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4 *>(a.part + at * HD + 16 * j + 4 * g) = acc[r][j];
+            if (g == 0) a.part_ml[at] = make_float2(mm[r], total);
+        } else if (i < live) {
+            const float inv = total == 0.f ? 0.f : kValueUnit<FMT> / total;
+            uint16_t *dst = out_row(a, place, first_row + i, HD) + 4 * g;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+                h4 res;
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) res[rr] = (_Float16)(acc[r][j][rr] * inv);
+                *reinterpret_cast<h4 *>(dst + 16 * j) = res;
+            }
+        }
+    }
+}
+
+// The parts of a sequence joined: a row to a workgroup, eight dimensions to a thread, the parts dealt to NT / CH threads and their sums
+// added in a fixed order.
+template <int HD>
+__global__ __launch_bounds__(NT) void tree_join(const TreeArgs a, float unit_v)
+{
+    constexpr int CH = HD / 8, LANES = NT / CH;
+    __shared__ float sums[LANES][HD + 4], totals[LANES];
+    const int bh = blockIdx.y, b = bh / a.nkv, row = blockIdx.x;
     if (row >= a.rows.fresh(b) * a.group) return;
-    const size_t first = (size_t)bh * a.splits * padded + row;
-    float m = kNone, total = 0.f, o[8] = {};
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[first + (size_t)s * padded].x);
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 x = a.part_ml[first + (size_t)s * padded];
+    const int part = threadIdx.x / CH, ch = threadIdx.x % CH;
+    const size_t first = (size_t)bh * a.splits * a.padded + row;
+    float m = kNone;
+    for (int s = threadIdx.x & 63; s < a.splits; s += 64) m = a.part_ml[first + (size_t)s * a.padded].x;      // (at most 64 parts)
+    m = cf::lanes::max_row(cf::lanes::max_groups<16>(m));
+    float total = 0.f, o[8] = {};
+    for (int s = part; s < a.splits; s += LANES) {
+        const float2 x = a.part_ml[first + (size_t)s * a.padded];
         const float f = exp2_(x.x - m);
-        const float4 *src = reinterpret_cast<const float4 *>(a.part + (first + (size_t)s * padded) * HD + d0);
+        const float4 *src = reinterpret_cast<const float4 *>(a.part + (first + (size_t)s * a.padded) * HD + 8 * ch);
         const float4 u = src[0], w = src[1];
         total += f * x.y;
         o[0] += f * u.x, o[1] += f * u.y, o[2] += f * u.z, o[3] += f * u.w;
         o[4] += f * w.x, o[5] += f * w.y, o[6] += f * w.z, o[7] += f * w.w;
     }
-    const float inv = total == 0.f ? 0.f : unit_v / total;
-    h8 res;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) res[e] = (_Float16)(o[e] * inv);
-    const int t = row / a.group, hh = row - t * a.group;
-    *reinterpret_cast<h8 *>(a.out + (((size_t)b * a.rows.tokens + t) * a.nq + head * a.group + hh) * HD + d0) = res;
+    for (int e = 0; e < 8; ++e) sums[part][8 * ch + e] = o[e];
+    if (ch == 0) totals[part] = total;
+    __syncthreads();
+    if (threadIdx.x < HD) {
+        float x = 0.f, all = 0.f;
+        const int lanes = min(a.splits, LANES);
+        for (int i = 0; i < lanes; ++i) x += sums[i][threadIdx.x], all += totals[i];
+        const Place at{a, bh};
+        out_row(a, at, row, HD)[threadIdx.x] = __builtin_bit_cast(uint16_t, (_Float16)(x * (all == 0.f ? 0.f : unit_v / all)));
+    }
 }
 
 using KernelFn = void (*)(const TreeArgs);
-template <int HD, int FMT>
-KernelFn pick_rows(int nr, bool forms)
-{
-    if (forms) return nr == 1 ? tree_tiles<HD, FMT, 1, true> : nr == 2 ? tree_tiles<HD, FMT, 2, true> : tree_tiles<HD, FMT, 4, true>;
-    return nr == 1 ? tree_tiles<HD, FMT, 1, false> : nr == 2 ? tree_tiles<HD, FMT, 2, false> : tree_tiles<HD, FMT, 4, false>;
-}
-KernelFn pick(int hd, int fmt, int nr, bool forms)
-{
-    if (hd == 64) return fmt == CF_CACHE_F16 ? pick_rows<64, CF_CACHE_F16>(nr, forms) : fmt == CF_CACHE_E4M3 ? pick_rows<64, CF_CACHE_E4M3>(nr, forms) : pick_rows<64, CF_CACHE_INT8>(nr, forms);
-    return fmt == CF_CACHE_F16 ? pick_rows<128, CF_CACHE_F16>(nr, forms) : fmt == CF_CACHE_E4M3 ? pick_rows<128, CF_CACHE_E4M3>(nr, forms) : pick_rows<128, CF_CACHE_INT8>(nr, forms);
-}
-
 // How a call is divided.
 struct Plan {
-    int nr, blocks, splits;
+    int shape;                     // index into kShapes
+    int blocks, splits;
 };
+// Rows of a workgroup: tree_tiles with one or two tiles of 16, tree_blocks with four wavefronts of one or two, or eight of two.  With
+// forms of the score one tile to a wavefront (more do not fit the registers).
+constexpr int kShapes = 5;
+struct Shape {
+    int rows, waves;
+};
+constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 4}, {128, 4}, {256, 8}}, kForms[kShapes] = {{16, 4}, {16, 4}, {64, 4}, {128, 8}, {128, 8}};
+
+template <int HD, int FMT, bool FORMS>
+KernelFn pick_shape(int shape)
+{
+    if constexpr (FORMS) {
+        return shape < 2 ? tree_tiles<HD, FMT, 1, true> : shape == 2 ? tree_blocks<HD, FMT, 4, 1, true> : tree_blocks<HD, FMT, 8, 1, true>;
+    } else {
+        static const KernelFn fn[kShapes] = {tree_tiles<HD, FMT, 1, false>, tree_tiles<HD, FMT, 2, false>, tree_blocks<HD, FMT, 4, 1, false>,
+                                             tree_blocks<HD, FMT, 4, 2, false>, tree_blocks<HD, FMT, 8, 2, false>};
+        return fn[shape];
+    }
+}
+template <int HD, bool FORMS>
+KernelFn pick_format(int fmt, int shape)
+{
+    return fmt == CF_CACHE_F16 ? pick_shape<HD, CF_CACHE_F16, FORMS>(shape) : fmt == CF_CACHE_E4M3 ? pick_shape<HD, CF_CACHE_E4M3, FORMS>(shape) : pick_shape<HD, CF_CACHE_INT8, FORMS>(shape);
+}
+KernelFn pick(int hd, int fmt, int shape, bool forms)
+{
+    if (hd == 64) return forms ? pick_format<64, true>(fmt, shape) : pick_format<64, false>(fmt, shape);
+    return forms ? pick_format<128, true>(fmt, shape) : pick_format<128, false>(fmt, shape);
+}
+
 constexpr int kMaxSplits = 64;
-// keys: the most that a row sees.  As many parts as bring two workgroups to a compute unit, with a step or more for every wavefront.
-Plan plan_of(int batch, int nkv, int group, int tokens, int keys, int cus, int limit)
+// keys: the most that a row sees.  As many parts as bring eight wavefronts to a compute unit, with a step or more for every wavefront.
+Plan plan_of(const Shape (&shapes)[kShapes], int batch, int nkv, int group, int tokens, int keys, int cus, int limit)
 {
     const int rows = tokens * group;
     Plan p;
-    p.nr = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.blocks = (rows + 16 * p.nr - 1) / (16 * p.nr);
-    const long long items = (long long)batch * nkv * p.blocks;
-    const int wanted = (int)((2ll * cus + items - 1) / items), most = (keys + NW * kStep - 1) / (NW * kStep);
+    for (p.shape = 0; p.shape < kShapes - 1 && rows > kPlain[p.shape].rows;) ++p.shape;
+    p.blocks = (rows + shapes[p.shape].rows - 1) / shapes[p.shape].rows;
+    const long long items = (long long)batch * nkv * p.blocks, slots = (long long)cus * 8 / shapes[p.shape].waves;
+    const int wanted = (int)((slots + items - 1) / items), least = p.shape < 2 ? NW * kStep : 2 * kBlockStep, most = (keys + least - 1) / least;
     p.splits = wanted < most ? wanted : most;
     if (p.splits > kMaxSplits) p.splits = kMaxSplits;
     if (limit > 0 && p.splits > limit) p.splits = limit;
@@ -453,9 +776,9 @@ int cf_tree_create(const cf_tree_config *cfg, cf_tree *out)
     if (hipGetDevice(&dev) != hipSuccess ||
         hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
         return CF_EHIP;
-    // Rows of partial results: a call with more than one part has fewer than 2 * cus + items workgroups of at most 64 rows, and items
-    // (batch rows, KV heads and row blocks) below 2 * cus.
-    const size_t rows = 4 * (size_t)cus * 64;
+    // Rows of partial results: a call with more than one part has fewer than twice as many workgroups as there are places for them, two
+    // to a compute unit up to 128 rows a workgroup, one with 256.
+    const size_t rows = 4 * (size_t)cus * 128;
     cf_tree t = new (std::nothrow) cf_tree_s();
     if (!t) return CF_ENOMEM;
     t->cfg = *cfg;
@@ -504,20 +827,22 @@ int cf_tree_attend(cf_tree t, int32_t batch, const void *q, const cf_cache *cach
     a.nq = c.n_q_heads, a.nkv = c.n_kv_heads, a.group = c.n_q_heads / c.n_kv_heads, a.max_seq = c.max_seq;
     a.window = t->cfg.window, a.cap = t->cfg.score_cap;
     const int keys = (a.window > 0 && a.window < draft->max_len ? a.window : draft->max_len) + draft->tokens;
-    Plan p = plan_of(batch, a.nkv, a.group, draft->tokens, keys, t->cus, t->max_splits);
-    const size_t rows = (size_t)batch * a.nkv * p.blocks * 16 * p.nr;
-    if (p.splits > 1 && rows * p.splits > t->ws_rows) p.splits = (int)(t->ws_rows / rows) > 1 ? (int)(t->ws_rows / rows) : 1;
+    const bool forms = a.cap > 0.f || a.window > 0 || a.slopes;
+    const auto &shapes = forms ? kForms : kPlain;
+    Plan p = plan_of(shapes, batch, a.nkv, a.group, draft->tokens, keys, t->cus, t->max_splits);
+    a.padded = p.blocks * shapes[p.shape].rows;
+    const size_t rows = (size_t)batch * a.nkv * a.padded;
+    if (rows * p.splits > t->ws_rows) p.splits = rows < t->ws_rows ? (int)(t->ws_rows / rows) : 1;
     a.splits = p.splits, a.blocks = p.blocks, a.units = batch * a.nkv * p.splits;
     a.part = reinterpret_cast<float *>(t->ws);
     a.part_ml = reinterpret_cast<float2 *>(t->ws + t->ws_rows * c.head_dim * sizeof(float));
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(pick(c.head_dim, c.format, p.nr, a.cap > 0.f || a.window > 0 || a.slopes), dim3((a.units + 7) / 8 * 8 * p.blocks), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL(pick(c.head_dim, c.format, p.shape, forms), dim3((a.units + 7) / 8 * 8 * p.blocks),
+                       dim3(64 * shapes[p.shape].waves), 0, s, a);
     if (hipGetLastError() != hipSuccess) return CF_EHIP;
     if (p.splits > 1) {
-        const int per = NT / (c.head_dim / 8), live = draft->tokens * a.group;
-        const float unit_v = c.format == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f;
-        hipLaunchKernelGGL((c.head_dim == 64 ? tree_join<64> : tree_join<128>), dim3((live + per - 1) / per, batch * a.nkv), dim3(NT), 0, s, a,
-                           p.blocks * 16 * p.nr, unit_v);
+        hipLaunchKernelGGL((c.head_dim == 64 ? tree_join<64> : tree_join<128>), dim3(draft->tokens * a.group, batch * a.nkv), dim3(NT), 0, s, a,
+                           c.format == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f);
         if (hipGetLastError() != hipSuccess) return CF_EHIP;
     }
     return CF_OK;

@@ -36,6 +36,22 @@ __device__ __forceinline__ uint32_t pair_of_e4m3(uint32_t x, bool high)
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// Eight codes as fp16.
+template <int FMT>
+__device__ __forceinline__ u32x4 widen(uint32_t a, uint32_t b)
+{
+    u32x4 o;
+    if constexpr (FMT == CF_CACHE_INT8) {
+        a ^= 0x80808080u, b ^= 0x80808080u;
+        o[0] = pair_of_int8(__builtin_amdgcn_perm(0u, a, 0x0c010c00u)), o[1] = pair_of_int8(__builtin_amdgcn_perm(0u, a, 0x0c030c02u));
+        o[2] = pair_of_int8(__builtin_amdgcn_perm(0u, b, 0x0c010c00u)), o[3] = pair_of_int8(__builtin_amdgcn_perm(0u, b, 0x0c030c02u));
+    } else {
+        o[0] = pair_of_e4m3(a, false), o[1] = pair_of_e4m3(a, true);
+        o[2] = pair_of_e4m3(b, false), o[3] = pair_of_e4m3(b, true);
+    }
+    return o;
+}
+
 // The keys of a step of 32: requested row by row, 16 bytes a load, used as A operands.
 template <int HD, int FMT>
 struct Keys {
@@ -58,20 +74,7 @@ struct Keys {
             return __builtin_bit_cast(h8, raw[t][ks]);
         } else {
             const u32x4 x = raw[t][ks / 2];
-            u32x4 o;
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                uint32_t q = x[2 * (ks & 1) + w];
-                if constexpr (FMT == CF_CACHE_INT8) {
-                    q ^= 0x80808080u;
-                    o[2 * w] = pair_of_int8(__builtin_amdgcn_perm(0u, q, 0x0c010c00u));
-                    o[2 * w + 1] = pair_of_int8(__builtin_amdgcn_perm(0u, q, 0x0c030c02u));
-                } else {
-                    o[2 * w] = pair_of_e4m3(q, false);
-                    o[2 * w + 1] = pair_of_e4m3(q, true);
-                }
-            }
-            return __builtin_bit_cast(h8, o);
+            return __builtin_bit_cast(h8, widen<FMT>(x[2 * (ks & 1)], x[2 * (ks & 1) + 1]));
         }
     }
 };
