@@ -35,7 +35,7 @@ constexpr int kStep = 32;                  // keys of a step
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;            // mm of a row that has seen nothing
 constexpr float kSmallScale = 0x1p-60f;    // stands for smaller scales: no fp16 result shows values of 448 times that
-constexpr float kMostWeight = 32768.f, kTopExponent = 7.f;
+constexpr float kMostWeight = 32768.f, kMoveFrom = 14.5f, kTopExponent = 7.f;
 
 struct TreeArgs {
     const uint16_t *q;
@@ -132,89 +132,120 @@ __device__ __forceinline__ float score_factor(float cap)
     return cap > 0.f ? unit * 2.f / cap : unit;                    // with a cap: twice its share of the cap, for the tanh
 }
 
-// The weights of a row for TILES tiles of 16 keys from j0 on, as B operands of the second product; moves the row's reference where
-// they ask for it.  MASKED: some row of the workgroup does not see all of these keys.
-template <int HD, int FMT, bool FORMS, bool MASKED, int TILES>
-__device__ __forceinline__ void weights(const TreeArgs &a, const Sequence &sq, const Row &row, int g, int j0, float to_score, const f32x4 (&s)[TILES],
-                                        const f32x4 (&kscale)[TILES], const f32x4 (&vscale)[TILES], float &mm, float &l, f32x4 (&acc)[HD / 16], h8 (&w)[TILES / 2])
+// Arguments x_j of a row for two tiles of 16 keys from j0 on; minus infinity for a key that it does not see.
+template <int FMT, bool FORMS>
+__device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq, const Row &row, int g, int j0, bool masked, float to_score,
+                                          const f32x4 (&s)[2], const f32x4 (&kscale)[2], float (&x)[8])
+{
+    const uint32_t bits = masked ? seen_bits(a, sq.tree, row.tok, j0, sq.len, sq.n) : ~0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = 16 * (e >> 2) + 4 * g + (e & 3), j = j0 + i;
+        x[e] = s[e >> 2][e & 3] * (FMT != CF_CACHE_F16 ? kscale[e >> 2][e & 3] : to_score);
+        bool seen = bits >> i & 1;
+        if constexpr (FORMS) {
+            int key_at = j;
+            if (masked) {
+                int new_at = sq.position(j - sq.len);
+                asm volatile("" : "+v"(new_at));                    // (no branch around the load)
+                key_at = j >= sq.len ? new_at : j;
+            }
+            const int distance = row.at - key_at;
+            if (a.cap > 0.f) x[e] = a.cap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(exp2_(x[e]) + 1.f));      // tanh
+            x[e] -= row.slope * (float)distance;
+            if (masked && a.window > 0) seen = seen && distance < a.window;
+        }
+        x[e] = seen ? x[e] : -INFINITY;
+    }
+}
+
+// What a row has summed so far.
+template <int HD>
+struct Sums {
+    float mm, l;
+    f32x4 acc[HD / 16];
+    __device__ __forceinline__ Sums() : mm(kNone), l(0.f)
+    {
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+};
+
+// The weights of NR rows for two tiles of 16 keys from j0 on, as B operands of the second product.  masked: some row of the workgroup does
+// not see all of these keys.  careful: some reference is so large that x_j - mm has to be the difference of rounded numbers (the fused
+// multiply-add keeps bits of x_j that mm, which was taken from a rounded one, lacks: above 2^24 that is whole powers of two).
+constexpr float kCareful = 0x1p20f;
+template <int HD, int FMT, bool FORMS, int NR>
+__device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, const Row (&row)[NR], int g, int j0, bool masked, bool &careful,
+                                      float to_score, const f32x4 (&s)[NR][2], const f32x4 (&kscale)[2], const f32x4 (&vscale)[2], Sums<HD> (&sum)[NR],
+                                      h8 (&w)[NR])
 {
     constexpr bool SCALED = FMT != CF_CACHE_F16;
-    constexpr int N = 4 * TILES;
-    float x[N], p[N], wt[N];
-    if constexpr (FORMS || MASKED) {
-        uint32_t bits = 0;
+    float add[NR];
+    for (int pass = 0;; ++pass) {
+        float most = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const int i = 16 * (e >> 2) + 4 * g + (e & 3), j = j0 + i;
-            if (MASKED && e % 8 == 0) bits = seen_bits(a, sq.tree, row.tok, j0 + 4 * e, sq.len, sq.n);
-            x[e] = s[e >> 2][e & 3] * (SCALED ? kscale[e >> 2][e & 3] : to_score);
-            bool seen = !MASKED || (bits >> (i & 31) & 1);
-            if constexpr (FORMS) {
-                int key_at = j;
-                if (MASKED) {
-                    const int new_at = sq.position(j - sq.len);
-                    key_at = j >= sq.len ? new_at : j;
+        for (int r = 0; r < NR; ++r) {
+            float p[8], wt[8];
+            if (FORMS || masked || careful) {
+                arguments<FMT, FORMS>(a, sq, row[r], g, j0, masked, to_score, s[r], kscale, p);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool none = p[e] == -INFINITY;
+                    p[e] = exp2_(p[e] - sum[r].mm);
+                    wt[e] = SCALED ? (none ? 0.f : p[e] * vscale[e >> 2][e & 3]) : p[e];       // (the scale of an unseen row may be anything)
                 }
-                const int distance = row.at - key_at;
-                if (a.cap > 0.f) x[e] = a.cap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(exp2_(x[e]) + 1.f));      // tanh
-                x[e] -= row.slope * (float)distance;
-                if (MASKED && a.window > 0) seen = seen && distance < a.window;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    p[e] = exp2_(fmaf(s[r][e >> 2][e & 3], SCALED ? kscale[e >> 2][e & 3] : to_score, -sum[r].mm));
+                    wt[e] = SCALED ? p[e] * vscale[e >> 2][e & 3] : p[e];
+                }
             }
-            if (!seen) x[e] = -INFINITY;
+            add[r] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+            most = fmaxf(fmaxf(most, wt[0]), wt[1]);
+#pragma unroll
+            for (int e = 2; e < 8; e += 2) most = fmaxf(fmaxf(most, wt[e]), wt[e + 1]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[r][e] = (_Float16)wt[e];
+        }
+        if (pass || !__any(most > kMostWeight)) break;
+        // some weight is too large: rows with such a one get a new reference, and all weights are taken again
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            float x[8], top = kNone, over = 0.f;
+            arguments<FMT, FORMS>(a, sq, row[r], g, j0, masked, to_score, s[r], kscale, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = x[e] == -INFINITY ? kNone : SCALED ? x[e] + __builtin_amdgcn_logf(vscale[e >> 2][e & 3]) : x[e];
+                top = fmaxf(top, y);
+            }
+            top = cf::lanes::max_groups<16>(top);
+            over = top - sum[r].mm;
+            const float to = over > kMoveFrom ? top - kTopExponent : sum[r].mm, by = exp2_(sum[r].mm - to);
+            sum[r].mm = to;
+            sum[r].l *= by;
+#pragma unroll
+            for (int j = 0; j < HD / 16; ++j) sum[r].acc[j] *= by;
+            careful = careful || __any(to > kCareful || (to < -kCareful && to != kNone));
         }
     }
-    auto weigh = [&]() {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            if constexpr (FORMS || MASKED)
-                p[e] = exp2_(x[e] - mm);
-            else
-                p[e] = exp2_(fmaf(s[e >> 2][e & 3], SCALED ? kscale[e >> 2][e & 3] : to_score, -mm));
-            wt[e] = SCALED ? p[e] * vscale[e >> 2][e & 3] : p[e];
-            if (SCALED && MASKED && x[e] == -INFINITY) wt[e] = 0.f;         // (the scale of an unseen row may be anything)
-        }
-    };
-    weigh();
-    float most = fmaxf(wt[0], wt[1]);
-#pragma unroll
-    for (int e = 2; e < N; e += 2) most = fmaxf(fmaxf(most, wt[e]), wt[e + 1]);
-    if (__any(most > kMostWeight)) {
-        float top = kNone;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            float y = FORMS || MASKED ? x[e] : s[e >> 2][e & 3] * (SCALED ? kscale[e >> 2][e & 3] : to_score);
-            if (SCALED) y += __builtin_amdgcn_logf(vscale[e >> 2][e & 3]);
-            top = fmaxf(top, MASKED && x[e] == -INFINITY ? kNone : y);
-        }
-        top = cf::lanes::max_groups<16>(top);
-        most = cf::lanes::max_groups<16>(most);
-        const float to = most > kMostWeight ? top - kTopExponent : mm, by = exp2_(mm - to);
-        mm = to;
-        l *= by;
-#pragma unroll
-        for (int j = 0; j < HD / 16; ++j) acc[j] *= by;
-        weigh();
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < N; e += 4) sum += (p[e] + p[e + 1]) + (p[e + 2] + p[e + 3]);
-    l += sum;
-#pragma unroll
-    for (int e = 0; e < N; ++e) w[e >> 3][e & 7] = (_Float16)wt[e];
+    for (int r = 0; r < NR; ++r) sum[r].l += add[r];
 }
 
 // Value rows with infinities or NaN that some row does not see would enter its product as 0 times that.  Where a step holds one, such
 // values are left out of the product, and this adds them, key by key, to the rows that see them.  dim(j, rr): dimension of acc[j][rr].
-template <int HD, int FMT, int TILES, typename Dim>
-__device__ __forceinline__ void add_unfit(__amdgpu_buffer_rsrc_t vr, int j0, int c, const h8 (&w)[TILES / 2], f32x4 (&acc)[HD / 16], Dim dim)
+template <int HD, int FMT, typename Dim>
+__device__ __forceinline__ void add_unfit(__amdgpu_buffer_rsrc_t vr, int j0, int c, const h8 &w, f32x4 (&acc)[HD / 16], Dim dim)
 {
     constexpr int ROW = HD * kValueBytes<FMT>;
 #pragma unroll 1
-    for (int i = 0; i < 16 * TILES; ++i) {
+    for (int i = 0; i < 32; ++i) {
         const int element = 4 * (i >> 4) + (i & 3);                 // key i is this element of lane group (i / 4) % 4
         float wt = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4 * TILES; ++e) wt = e == element ? (float)w[e >> 3][e & 7] : wt;
+        for (int e = 0; e < 8; ++e) wt = e == element ? (float)w[e] : wt;
         wt = __shfl(wt, 16 * ((i >> 2) & 3) + c);
 #pragma unroll
         for (int j = 0; j < HD / 16; ++j)
@@ -249,8 +280,8 @@ struct Part {
         int lo = 0;
         all_from = 0;
         if (FORMS && a.window > 0) {
-            lo = min(max(nearest - a.window + 1, 0), sq.len);
-            all_from = max(farthest - a.window + 1, 0);
+            lo = min(max(__builtin_amdgcn_readfirstlane(nearest) - a.window + 1, 0), sq.len);
+            all_from = max(__builtin_amdgcn_readfirstlane(farthest) - a.window + 1, 0);
         }
         const int first = lo / STEP, steps = (sq.end + STEP - 1) / STEP - first, per = (steps + a.splits - 1) / a.splits;
         begin = first + split * per, end = min(first + steps, begin + per);
@@ -307,7 +338,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     constexpr bool SCALED = FMT != CF_CACHE_F16;
     __shared__ float smem[NW * 16 * (HD + 4)];
     __shared__ float2 ml[NW][16 * NR];
-    __shared__ float scales[NW][2][kStep];
+    __shared__ alignas(16) float scales[NW][2][kStep];
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
     const Place place(a);
     if (place.unit >= a.units) return;
@@ -334,14 +365,8 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     Keys<HD, FMT> keys;
     Values<HD, FMT> vals;
     float scale = 0.f;
-    f32x4 acc[NR][NJ];
-    float mm[NR], l[NR];
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        mm[r] = kNone, l[r] = 0.f;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    Sums<HD> sum[NR];
+    bool careful = false;
     const uint32_t koff = Keys<HD, FMT>::offset(c, g), voff = Values<HD, FMT>::offset(c, g);
     auto load_scale = [&](int step) {
         if constexpr (SCALED) scale = scale_src[min(step * kStep + (lane & 31), sq.end - 1)];
@@ -382,15 +407,8 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
             wave_sync();
             load_scale(next);
         }
-        // ---- weights
-        h8 w[NR][1];
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            if (masked)
-                weights<HD, FMT, FORMS, true, 2>(a, sq, row[r], g, j0, to_score, s[r], kscale, vscale, mm[r], l[r], acc[r], w[r]);
-            else
-                weights<HD, FMT, FORMS, false, 2>(a, sq, row[r], g, j0, to_score, s[r], kscale, vscale, mm[r], l[r], acc[r], w[r]);
-        }
+        h8 w[NR];
+        weigh<HD, FMT, FORMS, NR>(a, sq, row, g, j0, masked, careful, to_score, s, kscale, vscale, sum, w);
         // ---- values
         h8 v[NJ];
         vals.operands(v);
@@ -409,21 +427,21 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
                     v[j] = __builtin_bit_cast(h8, x);
                 }
 #pragma unroll
-                for (int r = 0; r < NR; ++r) add_unfit<HD, FMT, 2>(vr, j0, c, w[r], acc[r], [&](int j, int rr) { return NJ * (4 * g + rr) + j; });
+                for (int r = 0; r < NR; ++r) add_unfit<HD, FMT>(vr, j0, c, w[r], sum[r].acc, [&](int j, int rr) { return NJ * (4 * g + rr) + j; });
             }
         }
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int r = 0; r < NR; ++r) acc[r][j] = mfma16(v[j], w[r][0], acc[r][j]);
+            for (int r = 0; r < NR; ++r) sum[r].acc[j] = mfma16(v[j], w[r], sum[r].acc[j]);
         vals.load(vr, voff + (uint32_t)next * (kStep * ROW));
     }
 
     // ---- the wavefronts' results joined, 16 rows at a time
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-        l[r] = cf::lanes::sum_groups<16>(l[r]);
-        if (g == 0) ml[wv][16 * r + c] = make_float2(mm[r], l[r]);
+        sum[r].l = cf::lanes::sum_groups<16>(sum[r].l);
+        if (g == 0) ml[wv][16 * r + c] = make_float2(sum[r].mm, sum[r].l);
     }
     constexpr int CH = HD / 8;                                      // a thread has eight dimensions of a row
     const int row16 = tid / CH, d0 = 8 * (tid % CH);
@@ -435,7 +453,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
 #pragma unroll
             for (int j = 0; j < NJ; j += 4)
                 *reinterpret_cast<float4 *>(smem + (wv * 16 + c) * (HD + 4) + NJ * (4 * g + rr) + j) =
-                    make_float4(acc[r][j][rr], acc[r][j + 1][rr], acc[r][j + 2][rr], acc[r][j + 3][rr]);
+                    make_float4(sum[r].acc[j][rr], sum[r].acc[j + 1][rr], sum[r].acc[j + 2][rr], sum[r].acc[j + 3][rr]);
         __syncthreads();
         const int i = 16 * r + row16;
         if (row16 < 16 && i < live) {
@@ -471,7 +489,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
 // sixteen rows of an operand start in different banks; a row of values 32 bytes, for the transposing reads of four rows by 16 dimensions.
 constexpr int kBlockStep = 64;
 template <int HD>
-struct Stage {
+struct alignas(16) Stage {
     static constexpr int KROW = 2 * HD + 16, VROW = 2 * HD + 32;
     char k[2][kBlockStep * KROW], v[2][kBlockStep * VROW];
     float scale[2][2][kBlockStep];
@@ -533,14 +551,8 @@ __global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
     const float *scale_src = SCALED ? (wv == 1 ? a.v_scale : a.k_scale) + slice : nullptr;
     const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
 
-    f32x4 acc[NR][NJ];
-    float mm[NR], l[NR];
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        mm[r] = kNone, l[r] = 0.f;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    Sums<HD> sum[NR];
+    bool careful = false;
 
     // ---- staging: requested a step ahead of the one that is written, which is a step ahead of the one that is used
     u32x4 kraw[PIECES], vraw[PIECES];
@@ -598,56 +610,51 @@ __global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
         if (my_rows >= live) continue;                              // a wavefront without rows only stages
         const int buf = (step - part.begin) & 1, j0 = step * kBlockStep;
         const char *kb = lds.k[buf], *vb = lds.v[buf];
-        f32x4 s[NR][4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const h8 k = *reinterpret_cast<const h8 *>(kb + (16 * t + c) * S::KROW + 64 * ks + 16 * g);
-#pragma unroll
-                for (int r = 0; r < NR; ++r) s[r][t] = mfma16(k, q[r][ks], ks ? s[r][t] : f32x4{0.f, 0.f, 0.f, 0.f});
-            }
-        f32x4 kscale[4], vscale[4];
-        if constexpr (SCALED) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                kscale[t] = *reinterpret_cast<const f32x4 *>(&lds.scale[buf][0][16 * t + 4 * g]);
-                vscale[t] = *reinterpret_cast<const f32x4 *>(&lds.scale[buf][1][16 * t + 4 * g]);
-            }
-        }
-        h8 w[NR][2];
         const bool masked = masked_step(step);
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            if (masked)
-                weights<HD, FMT, FORMS, true, 4>(a, sq, row[r], g, j0, to_score, s[r], kscale, vscale, mm[r], l[r], acc[r], w[r]);
-            else
-                weights<HD, FMT, FORMS, false, 4>(a, sq, row[r], g, j0, to_score, s[r], kscale, vscale, mm[r], l[r], acc[r], w[r]);
-        }
-        if (FMT != CF_CACHE_INT8 && masked && __builtin_amdgcn_readfirstlane(lds.unfit[buf]) == 1 + step)
+        for (int half = 0; half < 2; ++half) {
+            f32x4 s[NR][2];
 #pragma unroll
-            for (int r = 0; r < NR; ++r) add_unfit<HD, FMT, 4>(vr, j0, c, w[r], acc[r], [&](int j, int rr) { return 16 * j + 4 * g + rr; });
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+                for (int ks = 0; ks < KS; ++ks) {
+                    const h8 k = *reinterpret_cast<const h8 *>(kb + (32 * half + 16 * t + c) * S::KROW + 64 * ks + 16 * g);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
+                    for (int r = 0; r < NR; ++r) s[r][t] = mfma16(k, q[r][ks], ks ? s[r][t] : f32x4{0.f, 0.f, 0.f, 0.f});
+                }
+            f32x4 kscale[2], vscale[2];
+            if constexpr (SCALED) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    kscale[t] = *reinterpret_cast<const f32x4 *>(&lds.scale[buf][0][32 * half + 16 * t + 4 * g]);
+                    vscale[t] = *reinterpret_cast<const f32x4 *>(&lds.scale[buf][1][32 * half + 16 * t + 4 * g]);
+                }
+            }
+            h8 w[NR];
+            weigh<HD, FMT, FORMS, NR>(a, sq, row, g, j0 + 32 * half, masked, careful, to_score, s, kscale, vscale, sum, w);
+            if (FMT != CF_CACHE_INT8 && masked && __builtin_amdgcn_readfirstlane(lds.unfit[buf]) == 1 + step)
+#pragma unroll
+                for (int r = 0; r < NR; ++r) add_unfit<HD, FMT>(vr, j0 + 32 * half, c, w[r], sum[r].acc, [&](int j, int rr) { return 16 * j + 4 * g + rr; });
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
                 const h8 v = transposed<S::VROW>(vb, 32 * half, 16 * j, c, g);
 #pragma unroll
-                for (int r = 0; r < NR; ++r) acc[r][j] = mfma16(v, w[r][half], acc[r][j]);
+                for (int r = 0; r < NR; ++r) sum[r].acc[j] = mfma16(v, w[r], sum[r].acc[j]);
             }
+        }
     }
 
 #pragma unroll
-    for (int r = 0; r < NR; ++r) l[r] = cf::lanes::sum_groups<16>(l[r]);
+    for (int r = 0; r < NR; ++r) sum[r].l = cf::lanes::sum_groups<16>(sum[r].l);
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         const int i = my_rows + 16 * r + c;
-        const float total = l[r];
+        const float total = sum[r].l;
         if (i < live && a.splits > 1) {
             const size_t at = (size_t)place.unit * a.padded + first_row + i;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4 *>(a.part + at * HD + 16 * j + 4 * g) = acc[r][j];
-            if (g == 0) a.part_ml[at] = make_float2(mm[r], total);
+            for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4 *>(a.part + at * HD + 16 * j + 4 * g) = sum[r].acc[j];
+            if (g == 0) a.part_ml[at] = make_float2(sum[r].mm, total);
         } else if (i < live) {
             const float inv = total == 0.f ? 0.f : kValueUnit<FMT> / total;
             uint16_t *dst = out_row(a, place, first_row + i, HD) + 4 * g;
@@ -656,7 +663,7 @@ __global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
                 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
                 h4 res;
 #pragma unroll
-                for (int rr = 0; rr < 4; ++rr) res[rr] = (_Float16)(acc[r][j][rr] * inv);
+                for (int rr = 0; rr < 4; ++rr) res[rr] = (_Float16)(sum[r].acc[j][rr] * inv);
                 *reinterpret_cast<h4 *>(dst + 16 * j) = res;
             }
         }

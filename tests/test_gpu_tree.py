@@ -3,7 +3,7 @@ in draft_cases.bound."""
 import numpy as np
 import pytest
 
-from draft_cases import FORMATS, bound, bytes_code, cache_values, mask_words, random_tree
+from draft_cases import FORMATS, bound, bytes_code, cache_values, code_bytes, mask_words, random_tree
 from oracle import draft_block as orc
 
 torch = pytest.importorskip("torch")
@@ -249,6 +249,28 @@ def test_peaked_and_growing_scores(fmt, q_size):
         c.k[:] = (np.abs(c.k) * np.linspace(0, 1, c.rows)[:, None]).astype(np.float16)
         c.kv = c.k.astype(np.float64)
         c.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T", [1, 10, 40])
+@pytest.mark.parametrize("order", [1, -1])
+def test_scores_beyond_the_precision_of_one(fmt, T, order):
+    """Scores of 10^8 and more, where neighbouring fp32 numbers are several units apart: key j has the score (j + 1) times 3.8e6 (or the
+    other way round), so that the largest one takes all the weight, and the result is its value row: v w / w' with w the fp16 nearest to
+    w', off by half a step (2^-11) of w and of the result."""
+    c = Case(fmt, 4, 2, 64, [100], T, chain=True, seed=25)
+    c.q[:] = 60000
+    x = np.broadcast_to((8.0 * (np.arange(c.rows) + 1)[::order]).astype(np.float16)[:, None], (c.B, c.nkv, c.rows, 64))
+    if fmt == "f16":
+        c.k = np.ascontiguousarray(x)
+    else:
+        code, c.ks = orc.encode(x, fmt)
+        c.k = code_bytes(code, fmt)
+    got = c.run()
+    for t in range(T):
+        want = c.vv[0, :, 100 + t if order == 1 else 0]
+        for h in range(4):
+            assert (np.abs(got[0, t, h] - want[h // 2]) <= 2.0 ** -10 * 1.01 * np.abs(want[h // 2]) + 2.0 ** -25).all(), (t, h)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
