@@ -20,6 +20,7 @@
 #include <cmath>
 #include <cstring>
 #include <new>
+#include <type_traits>
 
 namespace {
 
@@ -42,8 +43,10 @@ struct TreeArgs {
     const char *k, *v;
     const float *k_scale, *v_scale, *slopes;
     uint16_t *out;
-    float *part;                   // [batch, KV head][split][row] : HD sums, for more than one split
-    float2 *part_ml;               // the same rows' mm and l
+    // for more than one part
+    float *part;                   // [batch, KV head][part][row]: HD sums, and behind all rows, from part_ml on, their mm and l
+    uint32_t part_ml, part_bytes;  // bytes
+    uint32_t *arrived;             // [batch, KV head][row block]: parts that are done, if the last one joins them; else NULL
     Lengths rows;
     const int32_t *depth;
     const uint64_t *tree;
@@ -330,6 +333,144 @@ __device__ __forceinline__ uint16_t *out_row(const TreeArgs &a, const Place &at,
 template <int FMT>
 constexpr float kValueUnit = FMT == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f;
 
+// ---- parts joined
+//
+// Partial results go through memory.  Either a second kernel joins them, or, where there is little to read, the workgroup whose part is done
+// last: the parts are then written through to memory (the dies' L2 caches are not coherent), a counter tells which workgroup is the last,
+// and that one reads past the caches.  Nobody waits for anybody.  (Written through, larger parts are slow: the 16-byte pieces do not meet in a
+// cache any more; 64 tokens over 4096 e4m3 rows in 16 parts 35 us, 23 with cached writes.)
+constexpr int kThrough = 16;       // cache policy: through to memory, from memory
+
+struct Partials {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t ml;
+    int hd;
+    __device__ __forceinline__ Partials(const TreeArgs &a, int hd) : r(cf::buffer_of(a.part, a.part_bytes)), ml(a.part_ml), hd(hd) {}
+    template <int AUX>
+    __device__ __forceinline__ void put(uint32_t row, int dim, const f32x4 &v) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, (row * hd + dim) * 4, 0, AUX);
+    }
+    template <int AUX>
+    __device__ __forceinline__ void put_ml(uint32_t row, float m, float l) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{__builtin_bit_cast(uint32_t, m), __builtin_bit_cast(uint32_t, l)}, r, ml + row * 8, 0, AUX);
+    }
+    template <int AUX>
+    __device__ __forceinline__ f32x4 get(uint32_t row, int dim) const
+    {
+        return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (row * hd + dim) * 4, 0, AUX));
+    }
+    template <int AUX>
+    __device__ __forceinline__ float2 get_ml(uint32_t row) const
+    {
+        return __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(r, ml + row * 8, 0, AUX));
+    }
+};
+
+// What T threads need to join rows.
+template <int HD, int T>
+struct JoinSpace {
+    float sums[T / (HD / 8)][HD + 4];
+    float2 ml[T / (HD / 8)];
+};
+// Rows first .. first + count - 1 of a sequence's head: eight dimensions of a row to a thread, its parts dealt to `lanes` (a power of two)
+// threads, whose sums are added in their order.
+template <int HD, int T, int AUX>
+__device__ __forceinline__ void join_rows(const TreeArgs &a, const Place &at, int first, int count, int lanes, float unit_v, JoinSpace<HD, T> &space)
+{
+    constexpr int CH = HD / 8, SLOTS = T / CH;
+    const Partials part(a, HD);
+    const int slot = threadIdx.x / CH, d0 = 8 * (threadIdx.x % CH), lane = slot & (lanes - 1), per_pass = SLOTS / lanes;
+    for (int r0 = 0; r0 < count; r0 += per_pass) {
+        const int row = first + min(r0 + slot / lanes, count - 1);
+        const uint32_t base = (uint32_t)at.bh * a.splits * a.padded + row;
+        float m = kNone, total = 0.f;
+        f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        auto fold = [&](auto deep) {                                // parts that are requested together
+            constexpr int DEEP = decltype(deep)::value;
+            for (int s = lane; s < a.splits; s += DEEP * lanes) {
+                float2 x[DEEP];
+                f32x4 u[DEEP][2];
+#pragma unroll
+                for (int i = 0; i < DEEP; ++i) {
+                    const uint32_t from = base + (uint32_t)min(s + i * lanes, a.splits - 1) * a.padded;
+                    x[i] = part.get_ml<AUX>(from);
+                    u[i][0] = part.get<AUX>(from, d0), u[i][1] = part.get<AUX>(from, d0 + 4);
+                }
+#pragma unroll
+                for (int i = 0; i < DEEP; ++i) {
+                    const bool there = s + i * lanes < a.splits;
+                    const float to = there ? fmaxf(m, x[i].x) : m, old = exp2_(m - to), f = there ? exp2_(x[i].x - to) : 0.f;
+                    m = to;
+                    total = total * old + (there ? f * x[i].y : 0.f);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) o[h] = o[h] * old + (there ? u[i][h] * f : f32x4{0.f, 0.f, 0.f, 0.f});
+                }
+            }
+        };
+        if (a.splits <= lanes)
+            fold(std::integral_constant<int, 1>());
+        else if (a.splits <= 2 * lanes)
+            fold(std::integral_constant<int, 2>());
+        else
+            fold(std::integral_constant<int, 4>());
+        if (lanes == 1) {
+            if (r0 + slot < count) {
+                const float inv = total == 0.f ? 0.f : unit_v / total;
+                h8 res;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) res[e] = (_Float16)(o[e >> 2][e & 3] * inv);
+                *reinterpret_cast<h8 *>(out_row(a, at, row, HD) + d0) = res;
+            }
+            continue;
+        }
+        if (r0) __syncthreads();
+        *reinterpret_cast<f32x4 *>(&space.sums[slot][d0]) = o[0];
+        *reinterpret_cast<f32x4 *>(&space.sums[slot][d0 + 4]) = o[1];
+        if (d0 == 0) space.ml[slot] = make_float2(m, total);
+        __syncthreads();
+        for (int i = threadIdx.x; i < min(per_pass, count - r0) * (HD / 4); i += T) {      // four dimensions of a row to a thread
+            const int mine = i / (HD / 4), d = 4 * (i % (HD / 4));
+            float top = kNone, sum = 0.f;
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            for (int s = 0; s < lanes; ++s) top = fmaxf(top, space.ml[mine * lanes + s].x);
+#pragma unroll 4
+            for (int s = 0; s < lanes; ++s) {
+                const float2 y = space.ml[mine * lanes + s];
+                const float f = exp2_(y.x - top);
+                sum += f * y.y;
+                x += *reinterpret_cast<const f32x4 *>(&space.sums[mine * lanes + s][d]) * f;
+            }
+            const float inv = sum == 0.f ? 0.f : unit_v / sum;
+            typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<h4 *>(out_row(a, at, first + r0 + mine, HD) + d) =
+                h4{(_Float16)(x[0] * inv), (_Float16)(x[1] * inv), (_Float16)(x[2] * inv), (_Float16)(x[3] * inv)};
+        }
+    }
+}
+// Whether this workgroup, whose partial results are on their way, is the last one of its row block; it clears the counter for the next launch.
+__device__ __forceinline__ bool last_to_arrive(const TreeArgs &a, const Place &at, int &shared)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                // this wavefront's results are in memory
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t *counter = a.arrived + at.bh * a.blocks + at.block;
+        const int before = (int)__hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == a.splits - 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        shared = before;
+    }
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(shared) == a.splits - 1;
+}
+// threads that share a row's parts
+__device__ __forceinline__ int join_lanes(int splits, int rows, int slots)
+{
+    int lanes = 1;
+    while (lanes < splits && 2 * lanes * rows <= slots) lanes *= 2;
+    return lanes;
+}
+
 // FORMS: the scores may be capped, biased or windowed.
 template <int HD, int FMT, int NR, bool FORMS>
 __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
@@ -469,11 +610,16 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
                 for (int e = 0; e < 8; ++e) o[e] += f * src[e];
             }
             if (a.splits > 1) {
-                const size_t at = (size_t)place.unit * a.padded + first_row + i;
-                float4 *dst = reinterpret_cast<float4 *>(a.part + at * HD + d0);
-                dst[0] = make_float4(o[0], o[1], o[2], o[3]);
-                dst[1] = make_float4(o[4], o[5], o[6], o[7]);
-                if (d0 == 0) a.part_ml[at] = make_float2(m, total);
+                const Partials to(a, HD);
+                const uint32_t at = (uint32_t)place.unit * a.padded + first_row + i;
+                const f32x4 lo = {o[0], o[1], o[2], o[3]}, hi = {o[4], o[5], o[6], o[7]};
+                if (a.arrived) {
+                    to.put<kThrough>(at, d0, lo), to.put<kThrough>(at, d0 + 4, hi);
+                    if (d0 == 0) to.put_ml<kThrough>(at, m, total);
+                } else {
+                    to.put<0>(at, d0, lo), to.put<0>(at, d0 + 4, hi);
+                    if (d0 == 0) to.put_ml<0>(at, m, total);
+                }
             } else {
                 const float inv = total == 0.f ? 0.f : kValueUnit<FMT> / total;
                 h8 res;
@@ -482,6 +628,11 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
                 *reinterpret_cast<h8 *>(out_row(a, place, first_row + i, HD) + d0) = res;
             }
         }
+    }
+    if (a.splits > 1 && a.arrived) {
+        __shared__ int before;
+        if (last_to_arrive(a, place, before))
+            join_rows<HD, NT, kThrough>(a, place, first_row, live, join_lanes(a.splits, live, NT / CH), kValueUnit<FMT>, *reinterpret_cast<JoinSpace<HD, NT> *>(smem));
     }
 }
 
@@ -651,10 +802,17 @@ __global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
         const int i = my_rows + 16 * r + c;
         const float total = sum[r].l;
         if (i < live && a.splits > 1) {
-            const size_t at = (size_t)place.unit * a.padded + first_row + i;
+            const Partials to(a, HD);
+            const uint32_t at = (uint32_t)place.unit * a.padded + first_row + i;
+            if (a.arrived) {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4 *>(a.part + at * HD + 16 * j + 4 * g) = sum[r].acc[j];
-            if (g == 0) a.part_ml[at] = make_float2(sum[r].mm, total);
+                for (int j = 0; j < NJ; ++j) to.put<kThrough>(at, 16 * j + 4 * g, sum[r].acc[j]);
+                if (g == 0) to.put_ml<kThrough>(at, sum[r].mm, total);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) to.put<0>(at, 16 * j + 4 * g, sum[r].acc[j]);
+                if (g == 0) to.put_ml<0>(at, sum[r].mm, total);
+            }
         } else if (i < live) {
             const float inv = total == 0.f ? 0.f : kValueUnit<FMT> / total;
             uint16_t *dst = out_row(a, place, first_row + i, HD) + 4 * g;
@@ -668,43 +826,22 @@ __global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
             }
         }
     }
+    if (a.splits > 1 && a.arrived) {
+        __shared__ int before;
+        static_assert(sizeof(JoinSpace<HD, T>) <= sizeof(S), "joined where the steps were");
+        if (last_to_arrive(a, place, before))
+            join_rows<HD, T, kThrough>(a, place, first_row, live, join_lanes(a.splits, live, T / (HD / 8)), kValueUnit<FMT>, *reinterpret_cast<JoinSpace<HD, T> *>(&lds));
+    }
 }
 
-// The parts of a sequence joined: a row to a workgroup, eight dimensions to a thread, the parts dealt to NT / CH threads and their sums
-// added in a fixed order.
+// The parts of a sequence joined by a kernel of its own: as many rows to a workgroup as its threads have.
 template <int HD>
-__global__ __launch_bounds__(NT) void tree_join(const TreeArgs a, float unit_v)
+__global__ __launch_bounds__(NT) void tree_join(const TreeArgs a, int lanes, float unit_v)
 {
-    constexpr int CH = HD / 8, LANES = NT / CH;
-    __shared__ float sums[LANES][HD + 4], totals[LANES];
-    const int bh = blockIdx.y, b = bh / a.nkv, row = blockIdx.x;
-    if (row >= a.rows.fresh(b) * a.group) return;
-    const int part = threadIdx.x / CH, ch = threadIdx.x % CH;
-    const size_t first = (size_t)bh * a.splits * a.padded + row;
-    float m = kNone;
-    for (int s = threadIdx.x & 63; s < a.splits; s += 64) m = a.part_ml[first + (size_t)s * a.padded].x;      // (at most 64 parts)
-    m = cf::lanes::max_row(cf::lanes::max_groups<16>(m));
-    float total = 0.f, o[8] = {};
-    for (int s = part; s < a.splits; s += LANES) {
-        const float2 x = a.part_ml[first + (size_t)s * a.padded];
-        const float f = exp2_(x.x - m);
-        const float4 *src = reinterpret_cast<const float4 *>(a.part + (first + (size_t)s * a.padded) * HD + 8 * ch);
-        const float4 u = src[0], w = src[1];
-        total += f * x.y;
-        o[0] += f * u.x, o[1] += f * u.y, o[2] += f * u.z, o[3] += f * u.w;
-        o[4] += f * w.x, o[5] += f * w.y, o[6] += f * w.z, o[7] += f * w.w;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sums[part][8 * ch + e] = o[e];
-    if (ch == 0) totals[part] = total;
-    __syncthreads();
-    if (threadIdx.x < HD) {
-        float x = 0.f, all = 0.f;
-        const int lanes = min(a.splits, LANES);
-        for (int i = 0; i < lanes; ++i) x += sums[i][threadIdx.x], all += totals[i];
-        const Place at{a, bh};
-        out_row(a, at, row, HD)[threadIdx.x] = __builtin_bit_cast(uint16_t, (_Float16)(x * (all == 0.f ? 0.f : unit_v / all)));
-    }
+    __shared__ JoinSpace<HD, NT> space;
+    const Place at(a, blockIdx.y);
+    const int per = NT / (HD / 8) / lanes, first = blockIdx.x * per, count = min(per, a.rows.fresh(at.b) * a.group - first);
+    if (count > 0) join_rows<HD, NT, 0>(a, at, first, count, lanes, unit_v, space);
 }
 
 using KernelFn = void (*)(const TreeArgs);
@@ -744,6 +881,8 @@ KernelFn pick(int hd, int fmt, int shape, bool forms)
 }
 
 constexpr int kMaxSplits = 64;
+// Partial values (fp32) that the last workgroup of a row block joins by itself.
+constexpr int kJoinedInPlace = 16384;
 // keys: the most that a row sees.  As many parts as bring eight wavefronts to a compute unit, with a step or more for every wavefront.
 Plan plan_of(const Shape (&shapes)[kShapes], int batch, int nkv, int group, int tokens, int keys, int cus, int limit)
 {
@@ -766,8 +905,9 @@ struct cf_tree_s {
     cf_tree_config cfg;
     int device = 0, cus = 0;
     int max_splits = 0;
-    char *ws = nullptr;
-    size_t ws_rows = 0;            // rows of partial results that the workspace holds
+    char *ws = nullptr;            // counters (zero between calls), then partial results
+    size_t ws_rows = 0;            // rows of partial results that it holds
+    uint32_t counters = 0;
 };
 
 extern "C" {
@@ -786,12 +926,17 @@ int cf_tree_create(const cf_tree_config *cfg, cf_tree *out)
     // Rows of partial results: a call with more than one part has fewer than twice as many workgroups as there are places for them, two
     // to a compute unit up to 128 rows a workgroup, one with 256.
     const size_t rows = 4 * (size_t)cus * 128;
+    const uint32_t counters = 4 * (uint32_t)cus;                    // row blocks of a call with more than one part: fewer than workgroups
     cf_tree t = new (std::nothrow) cf_tree_s();
     if (!t) return CF_ENOMEM;
     t->cfg = *cfg;
-    t->device = dev, t->cus = cus, t->ws_rows = rows;
-    const hipError_t e = hipMalloc(reinterpret_cast<void **>(&t->ws), rows * (cfg->cache.head_dim * sizeof(float) + sizeof(float2)));
+    t->device = dev, t->cus = cus, t->ws_rows = rows, t->counters = counters;
+    const size_t head = counters * sizeof(uint32_t);
+    hipError_t e = hipMalloc(reinterpret_cast<void **>(&t->ws), head + rows * (cfg->cache.head_dim * sizeof(float) + sizeof(float2)));
+    if (e == hipSuccess) e = hipMemset(t->ws, 0, head);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
+        if (t->ws) (void)hipFree(t->ws);
         delete t;
         return e == hipErrorOutOfMemory ? CF_ENOMEM : CF_EHIP;
     }
@@ -841,15 +986,22 @@ int cf_tree_attend(cf_tree t, int32_t batch, const void *q, const cf_cache *cach
     const size_t rows = (size_t)batch * a.nkv * a.padded;
     if (rows * p.splits > t->ws_rows) p.splits = rows < t->ws_rows ? (int)(t->ws_rows / rows) : 1;
     a.splits = p.splits, a.blocks = p.blocks, a.units = batch * a.nkv * p.splits;
-    a.part = reinterpret_cast<float *>(t->ws);
-    a.part_ml = reinterpret_cast<float2 *>(t->ws + t->ws_rows * c.head_dim * sizeof(float));
+    const size_t sums = t->ws_rows * c.head_dim * sizeof(float);
+    a.part = reinterpret_cast<float *>(t->ws + t->counters * sizeof(uint32_t));
+    a.part_ml = (uint32_t)sums, a.part_bytes = (uint32_t)(sums + t->ws_rows * sizeof(float2));
+    const int live = draft->tokens * a.group, block_rows = live < shapes[p.shape].rows ? live : shapes[p.shape].rows;
+    if (p.splits * block_rows * c.head_dim <= kJoinedInPlace && (uint32_t)batch * a.nkv * p.blocks <= t->counters)
+        a.arrived = reinterpret_cast<uint32_t *>(t->ws);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(pick(c.head_dim, c.format, p.shape, forms), dim3((a.units + 7) / 8 * 8 * p.blocks),
                        dim3(64 * shapes[p.shape].waves), 0, s, a);
     if (hipGetLastError() != hipSuccess) return CF_EHIP;
-    if (p.splits > 1) {
-        hipLaunchKernelGGL((c.head_dim == 64 ? tree_join<64> : tree_join<128>), dim3(draft->tokens * a.group, batch * a.nkv), dim3(NT), 0, s, a,
-                           c.format == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f);
+    if (p.splits > 1 && !a.arrived) {
+        const int slots = NT / (c.head_dim / 8);
+        int lanes = 1;
+        while (lanes < p.splits && lanes < slots) lanes *= 2;
+        hipLaunchKernelGGL((c.head_dim == 64 ? tree_join<64> : tree_join<128>), dim3((live * lanes + slots - 1) / slots, batch * a.nkv), dim3(NT), 0, s, a,
+                           lanes, c.format == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f);
         if (hipGetLastError() != hipSuccess) return CF_EHIP;
     }
     return CF_OK;
