@@ -659,11 +659,13 @@ __device__ __forceinline__ h8 transposed(const char *v, int first, int dim, int 
     return __builtin_bit_cast(h8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// WV wavefronts with 16 NR rows each share the steps of a part.
-template <int HD, int FMT, int WV, int NR, bool FORMS>
-__global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
+// RW wavefronts with 16 NR rows each share the steps of a part; with KG = 2 there are two such groups, one for each half of a step, whose
+// sums are joined at the end.  (One group needs 1.15 us for a step of 128 dimensions when it has the compute unit for itself, most of it
+// the time from one instruction to the next that needs its result.)
+template <int HD, int FMT, int RW, int KG, int NR, bool FORMS>
+__global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 {
-    constexpr int KS = HD / 32, NJ = HD / 16, ROW = HD * kValueBytes<FMT>, T = 64 * WV;
+    constexpr int WV = RW * KG, KS = HD / 32, NJ = HD / 16, ROW = HD * kValueBytes<FMT>, T = 64 * WV;
     constexpr bool SCALED = FMT != CF_CACHE_F16;
     // 16-byte pieces of a row; of the keys of a step, to a thread.  Where there are more threads than pieces the first ones have the keys,
     // the last ones the values.
@@ -675,9 +677,9 @@ __global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
     const Place place(a);
     if (place.unit >= a.units) return;
     const Sequence sq(a, place.b);
-    const int first_row = place.block * (16 * NR * WV), live = min(sq.n * a.group - first_row, 16 * NR * WV);
+    const int first_row = place.block * (16 * NR * RW), live = min(sq.n * a.group - first_row, 16 * NR * RW);
     if (live <= 0) return;
-    const int my_rows = 16 * NR * wv;                               // first of this wavefront's rows in the block
+    const int my_rows = 16 * NR * (wv % RW), my_half = wv / RW;     // first of this wavefront's rows in the block, its half of a step
 
     h8 q[NR][KS];
     Row row[NR];
@@ -763,7 +765,8 @@ __global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
         const char *kb = lds.k[buf], *vb = lds.v[buf];
         const bool masked = masked_step(step);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int h = 0; h < 2 / KG; ++h) {
+            const int half = KG == 2 ? my_half : h;
             f32x4 s[NR][2];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -797,9 +800,36 @@ __global__ __launch_bounds__(64 * WV, 2) void tree_blocks(const TreeArgs a)
 
 #pragma unroll
     for (int r = 0; r < NR; ++r) sum[r].l = cf::lanes::sum_groups<16>(sum[r].l);
+    if constexpr (KG == 2) {
+        constexpr int STRIDE = HD + 4;                              // floats of a row in LDS
+        float *other = reinterpret_cast<float *>(&lds);
+        float2 *other_ml = reinterpret_cast<float2 *>(other + 16 * NR * RW * STRIDE);
+        static_assert(16 * NR * RW * (STRIDE * sizeof(float) + sizeof(float2)) <= sizeof(S), "the second group's sums where the steps were");
+        __syncthreads();
+        if (my_half)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const int i = my_rows + 16 * r + c;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4 *>(other + i * STRIDE + 16 * j + 4 * g) = sum[r].acc[j];
+                other_ml[i] = make_float2(sum[r].mm, sum[r].l);     // (the same from all four lanes of a row)
+            }
+        __syncthreads();
+        if (!my_half)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const int i = my_rows + 16 * r + c;
+                const float2 x = other_ml[i];
+                const float to = fmaxf(sum[r].mm, x.x), mine = exp2_(sum[r].mm - to), theirs = exp2_(x.x - to);
+                sum[r].mm = to;
+                sum[r].l = sum[r].l * mine + x.y * theirs;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) sum[r].acc[j] = sum[r].acc[j] * mine + *reinterpret_cast<const f32x4 *>(other + i * STRIDE + 16 * j + 4 * g) * theirs;
+            }
+    }
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-        const int i = my_rows + 16 * r + c;
+        const int i = my_half ? live : my_rows + 16 * r + c;
         const float total = sum[r].l;
         if (i < live && a.splits > 1) {
             const Partials to(a, HD);
@@ -850,22 +880,22 @@ struct Plan {
     int shape;                     // index into kShapes
     int blocks, splits;
 };
-// Rows of a workgroup: tree_tiles with one or two tiles of 16, tree_blocks with four wavefronts of one or two, or eight of two.  With
-// forms of the score one tile to a wavefront (more do not fit the registers).
+// Rows of a workgroup: tree_tiles with one or two tiles of 16, tree_blocks with two groups of four wavefronts of one tile, four of two, or
+// eight of two.  With forms of the score one tile to a wavefront (more do not fit the registers).
 constexpr int kShapes = 5;
 struct Shape {
     int rows, waves;
 };
-constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 4}, {128, 4}, {256, 8}}, kForms[kShapes] = {{16, 4}, {16, 4}, {64, 4}, {128, 8}, {128, 8}};
+constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 8}, {128, 4}, {256, 8}}, kForms[kShapes] = {{16, 4}, {16, 4}, {64, 8}, {128, 8}, {128, 8}};
 
 template <int HD, int FMT, bool FORMS>
 KernelFn pick_shape(int shape)
 {
     if constexpr (FORMS) {
-        return shape < 2 ? tree_tiles<HD, FMT, 1, true> : shape == 2 ? tree_blocks<HD, FMT, 4, 1, true> : tree_blocks<HD, FMT, 8, 1, true>;
+        return shape < 2 ? tree_tiles<HD, FMT, 1, true> : shape == 2 ? tree_blocks<HD, FMT, 4, 2, 1, true> : tree_blocks<HD, FMT, 8, 1, 1, true>;
     } else {
-        static const KernelFn fn[kShapes] = {tree_tiles<HD, FMT, 1, false>, tree_tiles<HD, FMT, 2, false>, tree_blocks<HD, FMT, 4, 1, false>,
-                                             tree_blocks<HD, FMT, 4, 2, false>, tree_blocks<HD, FMT, 8, 2, false>};
+        static const KernelFn fn[kShapes] = {tree_tiles<HD, FMT, 1, false>, tree_tiles<HD, FMT, 2, false>, tree_blocks<HD, FMT, 4, 2, 1, false>,
+                                             tree_blocks<HD, FMT, 4, 1, 2, false>, tree_blocks<HD, FMT, 8, 1, 2, false>};
         return fn[shape];
     }
 }
