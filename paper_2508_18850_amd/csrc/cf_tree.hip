@@ -30,7 +30,7 @@ using cf::tree::Keys;
 using cf::tree::mfma16;
 using cf::tree::Values;
 
-constexpr int kMaxTokens = 256;
+constexpr int kMaxTokens = 256, kMaskWords = kMaxTokens / 64;
 constexpr int NT = 256, NW = NT / 64;
 constexpr int kStep = 32;                  // keys of a step
 constexpr float kLog2e = 1.4426950408889634f;
@@ -60,25 +60,28 @@ struct TreeArgs {
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return (uint32_t)(((1ull << min(max(n, 0), 32)) - 1)); }
 
-// Which of the keys j0 .. j0 + 31 token t sees: bit i for key j0 + i (without the window).  j0 is the same in all lanes; t < 0: none.
-__device__ __forceinline__ uint32_t seen_bits(const TreeArgs &a, const uint64_t *tree, int t, int j0, int len, int n)
+// Which of the keys j0 .. j0 + 31 token t sees: bit i for key j0 + i (without the window).  j0 is the same in all lanes; mask: the token's
+// words (t < 0: of any other token; it sees nothing).
+__device__ __forceinline__ uint32_t seen_bits(bool tree, int words, const uint64_t *mask, int t, int j0, int len, int n)
 {
     const int u0 = j0 - len;                                       // the new token at j0
     uint32_t mine = 0;
     if (!tree) {
         mine = low_bits(t - u0 + 1);
     } else if (u0 > -32) {
-        const uint64_t *w = tree + (size_t)max(t, 0) * a.words;
         const int i = max(u0, 0) >> 6, sh = max(u0, 0) & 63;
-        if (i < a.words) {
-            uint64_t x = w[i] >> sh;
-            if (sh > 32 && i + 1 < a.words) x |= w[i + 1] << (64 - sh);
+        if (i < words) {
+            uint64_t x = mask[i] >> sh;
+            if (sh > 32 && i + 1 < words) x |= mask[i + 1] << (64 - sh);
             mine = (uint32_t)x << max(-u0, 0);
         }
     }
     const uint32_t seen = (low_bits(len - j0) | (mine & ~low_bits(-u0))) & low_bits(len + n - j0);
     return t < 0 ? 0u : seen;
 }
+
+// the scale of a row of values, not below kSmallScale (a NaN stays one; scales are not negative)
+__device__ __forceinline__ float at_least_small(float x) { return x != x ? x : fmaxf(x, kSmallScale); }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -111,18 +114,24 @@ struct Sequence {
           tree(a.tree ? a.tree + (size_t)b * a.tree_stride : nullptr)
     {
     }
-    // of new token u (taken into 0 .. n - 1); kept where differences do not overflow
+    // of new token u; kept where differences do not overflow
     __device__ __forceinline__ int position(int u) const
     {
-        u = min(max(u, 0), n - 1);
         const int p = __builtin_elementwise_add_sat(len, depth ? depth[u] : u);
         return min(max(p, -kFar), kFar);
     }
 };
 
+// What the workgroups that have new tokens among their keys look up in LDS: the masks of their rows, the positions of the new tokens.
+template <int ROWS>
+struct Lookup {
+    uint64_t mask[ROWS][kMaskWords];
+    int at[kMaxTokens];
+};
 // One row of queries of a lane.
 struct Row {
     int tok;                       // its token, -1: padding
+    const uint64_t *mask;          // its words, in LDS
     int at;                        // position and slope (times log2 e): with FORMS
     float slope;
 };
@@ -137,10 +146,10 @@ __device__ __forceinline__ float score_factor(float cap)
 
 // Arguments x_j of a row for two tiles of 16 keys from j0 on; minus infinity for a key that it does not see.
 template <int FMT, bool FORMS>
-__device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq, const Row &row, int g, int j0, bool masked, float to_score,
+__device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row &row, int g, int j0, bool masked, float to_score,
                                           const f32x4 (&s)[2], const f32x4 (&kscale)[2], float (&x)[8])
 {
-    const uint32_t bits = masked ? seen_bits(a, sq.tree, row.tok, j0, sq.len, sq.n) : ~0u;
+    const uint32_t bits = masked ? seen_bits(sq.tree != nullptr, a.words, row.mask, row.tok, j0, sq.len, sq.n) : ~0u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int i = 16 * (e >> 2) + 4 * g + (e & 3), j = j0 + i;
@@ -149,9 +158,9 @@ __device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq,
         if constexpr (FORMS) {
             int key_at = j;
             if (masked) {
-                int new_at = sq.position(j - sq.len);
-                asm volatile("" : "+v"(new_at));                    // (no branch around the load)
-                key_at = j >= sq.len ? new_at : j;
+                int theirs = new_at[min(max(j - sq.len, 0), sq.n - 1)];
+                asm volatile("" : "+v"(theirs));                    // (no branch around the load)
+                key_at = j >= sq.len ? theirs : j;
             }
             const int distance = row.at - key_at;
             if (a.cap > 0.f) x[e] = a.cap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(exp2_(x[e]) + 1.f));      // tanh
@@ -179,7 +188,7 @@ struct Sums {
 // multiply-add keeps bits of x_j that mm, which was taken from a rounded one, lacks: above 2^24 that is whole powers of two).
 constexpr float kCareful = 0x1p20f;
 template <int HD, int FMT, bool FORMS, int NR>
-__device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, const Row (&row)[NR], int g, int j0, bool masked, bool &careful,
+__device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row (&row)[NR], int g, int j0, bool masked, bool &careful,
                                       float to_score, const f32x4 (&s)[NR][2], const f32x4 (&kscale)[2], const f32x4 (&vscale)[2], Sums<HD> (&sum)[NR],
                                       h8 (&w)[NR])
 {
@@ -191,7 +200,7 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
         for (int r = 0; r < NR; ++r) {
             float p[8], wt[8];
             if (FORMS || masked || careful) {
-                arguments<FMT, FORMS>(a, sq, row[r], g, j0, masked, to_score, s[r], kscale, p);
+                arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], kscale, p);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const bool none = p[e] == -INFINITY;
@@ -217,7 +226,7 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             float x[8], top = kNone, over = 0.f;
-            arguments<FMT, FORMS>(a, sq, row[r], g, j0, masked, to_score, s[r], kscale, x);
+            arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], kscale, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float y = x[e] == -INFINITY ? kNone : SCALED ? x[e] + __builtin_amdgcn_logf(vscale[e >> 2][e & 3]) : x[e];
@@ -307,11 +316,11 @@ struct Place {
 
 // Queries of a row as B operands (dims(ks): first dimension of this lane's eight in contraction step ks) and what else a row has.
 template <int HD, bool FORMS, typename Dims>
-__device__ __forceinline__ Row load_row(const TreeArgs &a, const Sequence &sq, const Place &at, int index, h8 (&q)[HD / 32], int &nearest, int &farthest, Dims dims)
+__device__ __forceinline__ Row load_row(const TreeArgs &a, const Sequence &sq, const Place &at, int index, const uint64_t *mask, h8 (&q)[HD / 32], int &nearest, int &farthest, Dims dims)
 {
     const bool there = index / a.group < sq.n;
     const int from = min(index, sq.n * a.group - 1), t = from / a.group, hh = from - t * a.group;
-    Row row = {there ? t : -1, 0, 0.f};
+    Row row = {there ? t : -1, mask, 0, 0.f};
     const uint16_t *src = a.q + (((size_t)at.b * a.rows.tokens + t) * a.nq + at.head * a.group + hh) * HD;
 #pragma unroll
     for (int ks = 0; ks < HD / 32; ++ks) {
@@ -324,6 +333,18 @@ __device__ __forceinline__ Row load_row(const TreeArgs &a, const Sequence &sq, c
         nearest = min(nearest, row.at), farthest = max(farthest, row.at);      // (a row of padding repeats the last one)
     }
     return row;
+}
+// Fills the rows first .. first + live - 1 of a Lookup; a barrier has to follow.
+template <bool FORMS, int T, int ROWS>
+__device__ __forceinline__ void fill(const TreeArgs &a, const Sequence &sq, int first, int live, Lookup<ROWS> &look_up)
+{
+    if (sq.tree)
+        for (int i = threadIdx.x; i < live * a.words; i += T) {
+            const int r = i / a.words, w = i - r * a.words;
+            look_up.mask[r][w] = sq.tree[(size_t)((first + r) / a.group) * a.words + w];
+        }
+    if (FORMS)
+        for (int u = threadIdx.x; u < sq.n; u += T) look_up.at[u] = sq.position(u);
 }
 __device__ __forceinline__ uint16_t *out_row(const TreeArgs &a, const Place &at, int index, int hd)
 {
@@ -479,6 +500,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     constexpr bool SCALED = FMT != CF_CACHE_F16;
     __shared__ float smem[NW * 16 * (HD + 4)];
     __shared__ float2 ml[NW][16 * NR];
+    __shared__ Lookup<16 * NR> look_up;
     __shared__ alignas(16) float scales[NW][2][kStep];
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
     const Place place(a);
@@ -492,7 +514,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     int nearest = kFar, farthest = -kFar;                           // of the positions of the block's tokens
 #pragma unroll
     for (int r = 0; r < NR; ++r)
-        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + 16 * r + c, q[r], nearest, farthest, [&](int ks) { return Keys<HD, FMT>::dim(ks, g); });
+        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + 16 * r + c, look_up.mask[16 * r + c], q[r], nearest, farthest, [&](int ks) { return Keys<HD, FMT>::dim(ks, g); });
     if (FORMS && a.window > 0)
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
@@ -518,12 +540,16 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
         keys.load(kr, koff + (uint32_t)step * (kStep * ROW));
         vals.load(vr, voff + (uint32_t)step * (kStep * ROW));
     }
+    if (part.end * kStep > sq.len) {
+        fill<FORMS, NT>(a, sq, first_row, live, look_up);
+        lds_barrier();
+    }
     for (; step < part.end; step += NW) {
         const int j0 = step * kStep;
         const bool masked = j0 + kStep > sq.len || j0 < part.all_from;      // (the same for the whole wavefront)
         const int next = min(step + NW, part.end - 1);
         if constexpr (SCALED) {
-            const float x = lane < 32 ? scale * to_score : fabsf(scale) < kSmallScale ? kSmallScale : scale;
+            const float x = lane < 32 ? scale * to_score : at_least_small(scale);
             scales[wv][lane >> 5][lane & 31] = x;
         }
         // ---- scores
@@ -549,7 +575,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
             load_scale(next);
         }
         h8 w[NR];
-        weigh<HD, FMT, FORMS, NR>(a, sq, row, g, j0, masked, careful, to_score, s, kscale, vscale, sum, w);
+        weigh<HD, FMT, FORMS, NR>(a, sq, look_up.at, row, g, j0, masked, careful, to_score, s, kscale, vscale, sum, w);
         // ---- values
         h8 v[NJ];
         vals.operands(v);
@@ -647,13 +673,18 @@ struct alignas(16) Stage {
     int unfit[2];                  // 1 + the step of this buffer that holds infinities or NaN among its values
 };
 
+// A row's 16-byte chunks (eight dimensions) in LDS: those of the second half of 128 dimensions change places in pairs.  The eight lanes that
+// write a row of 8-bit values, two chunks each, then write to all 32 banks at a time and not twice to every other four.
+__device__ __forceinline__ int chunk_at(int chunk) { return chunk ^ (chunk >> 3 & 1); }
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 // A operand of 16 dimensions from dim on and the keys of one h8 of weights: of keys first + 4 g .. + 3 and first + 16 + 4 g .. + 3.
 template <int VROW>
 __device__ __forceinline__ h8 transposed(const char *v, int first, int dim, int c, int g)
 {
     using Ptr = __attribute__((address_space(3))) s16x4 *;
-    const char *at = v + (first + 4 * g + (c >> 2)) * VROW + 2 * (dim + 4 * (c & 3));
+    const int of_row = dim < 64 ? c & 3 : (c & 3) ^ 2;              // (dim is a constant, chunk_at of dim / 8 + (c & 3) / 2)
+    const char *at = v + (first + 4 * g + (c >> 2)) * VROW + 2 * (dim + 4 * of_row);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(at + 16 * VROW));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(h8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -673,6 +704,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     static_assert(ALL % T == 0 || 2 * ALL == T, "every thread stages as much");
     using S = Stage<HD>;
     __shared__ S lds;
+    __shared__ Lookup<16 * NR * RW> look_up;
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
     const Place place(a);
     if (place.unit >= a.units) return;
@@ -686,7 +718,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     int nearest = kFar, farthest = -kFar;
 #pragma unroll
     for (int r = 0; r < NR; ++r)
-        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + my_rows + 16 * r + c, q[r], nearest, farthest, [&](int ks) { return 32 * ks + 8 * g; });
+        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + my_rows + 16 * r + c, look_up.mask[my_rows + 16 * r + c], q[r], nearest, farthest, [&](int ks) { return 32 * ks + 8 * g; });
     if (FORMS && a.window > 0) {                                    // the part is the whole block's: its extremes by way of LDS
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
@@ -726,7 +758,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         const bool look = FMT != CF_CACHE_INT8 && masked_step(step);
         uint32_t odd = 0;
         auto put = [&](char *rows, int row_bytes, const u32x4 &raw, int piece, bool check) {
-            char *dst = rows + piece / PPR * row_bytes + piece % PPR * (FMT == CF_CACHE_F16 ? 16 : 32);
+            char *dst = rows + piece / PPR * row_bytes;
+            const int col = piece % PPR;
 #pragma unroll
             for (int half = 0; half < (FMT == CF_CACHE_F16 ? 1 : 2); ++half) {
                 u32x4 x = raw;
@@ -734,7 +767,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
                 if (check)
 #pragma unroll
                     for (int d = 0; d < 4; ++d) odd |= unfit_bits(x[d]), x[d] = without_unfit(x[d]);
-                *reinterpret_cast<u32x4 *>(dst + 16 * half) = x;
+                *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(FMT == CF_CACHE_F16 ? col : 2 * col + half)) = x;
             }
         };
         if (!APART || 64 * wv < ALL)
@@ -745,12 +778,13 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
             for (int i = 0; i < PIECES; ++i) put(lds.v[buf], S::VROW, vraw[i], tid + T * i - APART, look);
         if (look && __any(odd)) lds.unfit[buf] = 1 + step;
         if (SCALED && wv < 2)
-            lds.scale[buf][wv][lane] = wv == 0 ? scale * to_score : fabsf(scale) < kSmallScale ? kSmallScale : scale;
+            lds.scale[buf][wv][lane] = wv == 0 ? scale * to_score : at_least_small(scale);
     };
     if (tid < 2) lds.unfit[tid] = 0;
-    __syncthreads();
     if (part.begin < part.end) {
         request(part.begin);
+        if (part.end * kBlockStep > sq.len) fill<FORMS, T>(a, sq, first_row, live, look_up);
+        lds_barrier();
         write(part.begin);
         request(min(part.begin + 1, part.end - 1));
     }
@@ -772,7 +806,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    const h8 k = *reinterpret_cast<const h8 *>(kb + (32 * half + 16 * t + c) * S::KROW + 64 * ks + 16 * g);
+                    const h8 k = *reinterpret_cast<const h8 *>(kb + (32 * half + 16 * t + c) * S::KROW + 64 * ks + 16 * (ks < 2 ? g : g ^ 1));
 #pragma unroll
                     for (int r = 0; r < NR; ++r) s[r][t] = mfma16(k, q[r][ks], ks ? s[r][t] : f32x4{0.f, 0.f, 0.f, 0.f});
                 }
@@ -785,7 +819,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
                 }
             }
             h8 w[NR];
-            weigh<HD, FMT, FORMS, NR>(a, sq, row, g, j0 + 32 * half, masked, careful, to_score, s, kscale, vscale, sum, w);
+            weigh<HD, FMT, FORMS, NR>(a, sq, look_up.at, row, g, j0 + 32 * half, masked, careful, to_score, s, kscale, vscale, sum, w);
             if (FMT != CF_CACHE_INT8 && masked && __builtin_amdgcn_readfirstlane(lds.unfit[buf]) == 1 + step)
 #pragma unroll
                 for (int r = 0; r < NR; ++r) add_unfit<HD, FMT>(vr, j0 + 32 * half, c, w[r], sum[r].acc, [&](int j, int rr) { return 16 * j + 4 * g + rr; });
