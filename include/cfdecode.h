@@ -424,7 +424,7 @@ int64_t cf_ffn_algorithmic_bytes(const cf_ffn_config *cfg, int32_t batch);
  *   CF_CACHE_F16    fp16 (the tensors that cf_decode_block and cf_decode_layer take; no scales)
  *   CF_CACHE_E4M3   8-bit floats (OCP e4m3: 448 is the largest) and one fp32 scale for every cached row of a head,
  *   CF_CACHE_INT8   8-bit integers (-127..127)                  scales [batch, n_kv_heads, max_seq]; a value is code * scale
- * A row (head_dim fp16 values) is held in 8 bits as  scale = top / Q  and  code = x * Q / top  rounded to the nearest code, ties
+ * (at least 0; what these calls write is).  A row (head_dim fp16 values) is held in 8 bits as  scale = top / Q  and  code = x * Q / top  rounded to the nearest code, ties
  * to even, where top is the row's largest magnitude and Q = 448 or 127; the code is the correctly rounded one.  A row of zeros has
  * scale 0 and codes 0; a row that holds an infinity or a NaN has scale NaN and codes 0, so that all of it reads back as NaN.
  */

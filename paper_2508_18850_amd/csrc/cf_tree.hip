@@ -276,34 +276,10 @@ __device__ __forceinline__ void add_unfit(__amdgpu_buffer_rsrc_t vr, int j0, int
             }
     }
 }
-__device__ __forceinline__ uint32_t unfit_bits(uint32_t pair) { return ((pair & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
-__device__ __forceinline__ uint32_t without_unfit(uint32_t pair)
-{
-    const uint32_t bad = unfit_bits(pair);
-    return pair & ~((bad >> 15) * 0xffffu);
-}
-
-// Keys of a part in steps of STEP, counted from key 0, and from which key on all rows of the workgroup see all cached rows.
-template <bool FORMS, int STEP>
-struct Part {
-    int begin, end, all_from;
-    __device__ __forceinline__ Part(const TreeArgs &a, const Sequence &sq, int split, int nearest, int farthest)
-    {
-        int lo = 0;
-        all_from = 0;
-        if (FORMS && a.window > 0) {
-            lo = min(max(__builtin_amdgcn_readfirstlane(nearest) - a.window + 1, 0), sq.len);
-            all_from = max(__builtin_amdgcn_readfirstlane(farthest) - a.window + 1, 0);
-        }
-        const int first = lo / STEP, steps = (sq.end + STEP - 1) / STEP - first, per = (steps + a.splits - 1) / a.splits;
-        begin = first + split * per, end = min(first + steps, begin + per);
-    }
-};
-
 // Where a workgroup works: workgroup i runs on die i mod 8, and the row blocks of a unit (a sequence's head and part), which read the same
 // keys and values, follow each other on one die.
 struct Place {
-    int unit, block, bh, split, b, head;
+    int unit, block, bh, split, b, head;                           // bh: batch row and KV head
     __device__ __forceinline__ explicit Place(const TreeArgs &a)
     {
         const int turn = blockIdx.x >> 3;
@@ -312,6 +288,23 @@ struct Place {
         b = bh / a.nkv, head = bh - b * a.nkv;
     }
     __device__ __forceinline__ Place(const TreeArgs &a, int bh) : unit(0), block(0), bh(bh), split(0), b(bh / a.nkv), head(bh % a.nkv) {}
+};
+
+// Keys of a part in steps of STEP, counted from key 0, and from which key on all rows of the workgroup see all cached rows.
+template <bool FORMS, int STEP>
+struct Part {
+    int begin, end, all_from;
+    __device__ __forceinline__ Part(const TreeArgs &a, const Sequence &sq, const Place &at, int nearest, int farthest)
+    {
+        int lo = 0;
+        all_from = 0;
+        if (FORMS && a.window > 0) {
+            lo = min(max(__builtin_amdgcn_readfirstlane(nearest) - a.window + 1, 0), sq.len);
+            all_from = max(__builtin_amdgcn_readfirstlane(farthest) - a.window + 1, 0);
+        }
+        const int first = lo / STEP, steps = (sq.end + STEP - 1) / STEP - first, per = (steps + a.splits - 1) / a.splits;
+        begin = first + at.split * per, end = min(first + steps, begin + per);
+    }
 };
 
 // Queries of a row as B operands (dims(ks): first dimension of this lane's eight in contraction step ks) and what else a row has.
@@ -518,7 +511,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     if (FORMS && a.window > 0)
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
-    const Part<FORMS, kStep> part(a, sq, place.split, nearest, farthest);
+    const Part<FORMS, kStep> part(a, sq, place, nearest, farthest);
 
     const size_t slice = (size_t)place.bh * a.max_seq;
     const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
@@ -577,30 +570,19 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
         h8 w[NR];
         weigh<HD, FMT, FORMS, NR>(a, sq, look_up.at, row, g, j0, masked, careful, to_score, s, kscale, vscale, sum, w);
         // ---- values
-        h8 v[NJ];
-        vals.operands(v);
-        if (FMT != CF_CACHE_INT8 && masked) {
-            uint32_t odd = 0;
+        if (FMT != CF_CACHE_INT8 && masked && __any(vals.take_out_unfit()))
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
+            for (int r = 0; r < NR; ++r) add_unfit<HD, FMT>(vr, j0, c, w[r], sum[r].acc, [&](int j, int rr) { return NJ * (4 * g + rr) + j; });
+        vals.flip();
 #pragma unroll
-                for (int d = 0; d < 4; ++d) odd |= unfit_bits(__builtin_bit_cast(cf::tree::u32x4, v[j])[d]);
-            if (__any(odd)) {
+        for (int pair = 0; pair < NJ / 2; ++pair) {
+            h8 v[2];
+            vals.operands(pair, v);
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    cf::tree::u32x4 x = __builtin_bit_cast(cf::tree::u32x4, v[j]);
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) x[d] = without_unfit(x[d]);
-                    v[j] = __builtin_bit_cast(h8, x);
-                }
-#pragma unroll
-                for (int r = 0; r < NR; ++r) add_unfit<HD, FMT>(vr, j0, c, w[r], sum[r].acc, [&](int j, int rr) { return NJ * (4 * g + rr) + j; });
-            }
+                for (int r = 0; r < NR; ++r) sum[r].acc[2 * pair + j] = mfma16(v[j], w[r], sum[r].acc[2 * pair + j]);
         }
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int r = 0; r < NR; ++r) sum[r].acc[j] = mfma16(v[j], w[r], sum[r].acc[j]);
         vals.load(vr, voff + (uint32_t)next * (kStep * ROW));
     }
 
@@ -729,7 +711,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         for (int i = 0; i < WV; ++i) nearest = min(nearest, ends[2 * i]), farthest = max(farthest, ends[2 * i + 1]);
         __syncthreads();
     }
-    const Part<FORMS, kBlockStep> part(a, sq, place.split, nearest, farthest);
+    const Part<FORMS, kBlockStep> part(a, sq, place, nearest, farthest);
 
     const size_t slice = (size_t)place.bh * a.max_seq;
     const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
@@ -757,17 +739,17 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         const int buf = (step - part.begin) & 1;
         const bool look = FMT != CF_CACHE_INT8 && masked_step(step);
         uint32_t odd = 0;
-        auto put = [&](char *rows, int row_bytes, const u32x4 &raw, int piece, bool check) {
+        auto put = [&](char *rows, int row_bytes, u32x4 raw, int piece, bool check) {
+            if (check)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) odd |= cf::tree::unfit_bits<FMT>(raw[d]), raw[d] = cf::tree::without_unfit<FMT>(raw[d]);
             char *dst = rows + piece / PPR * row_bytes;
             const int col = piece % PPR;
-#pragma unroll
-            for (int half = 0; half < (FMT == CF_CACHE_F16 ? 1 : 2); ++half) {
-                u32x4 x = raw;
-                if constexpr (FMT != CF_CACHE_F16) x = cf::tree::widen<FMT>(raw[2 * half], raw[2 * half + 1]);
-                if (check)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) odd |= unfit_bits(x[d]), x[d] = without_unfit(x[d]);
-                *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(FMT == CF_CACHE_F16 ? col : 2 * col + half)) = x;
+            if constexpr (FMT == CF_CACHE_F16) {
+                *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(col)) = raw;
+            } else {
+                *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(2 * col)) = cf::tree::widen<FMT>(raw[0], raw[1]);
+                *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(2 * col + 1)) = cf::tree::widen<FMT>(raw[2], raw[3]);
             }
         };
         if (!APART || 64 * wv < ALL)
@@ -920,13 +902,15 @@ constexpr int kShapes = 5;
 struct Shape {
     int rows, waves;
 };
-constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 8}, {128, 4}, {256, 8}}, kForms[kShapes] = {{16, 4}, {16, 4}, {64, 8}, {128, 8}, {128, 8}};
+constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 8}, {128, 4}, {256, 8}}, kPlain8[kShapes] = {{16, 4}, {32, 4}, {32, 4}, {32, 4}, {256, 8}}, kForms[kShapes] = {{16, 4}, {16, 4}, {64, 8}, {128, 8}, {128, 8}};
 
 template <int HD, int FMT, bool FORMS>
 KernelFn pick_shape(int shape)
 {
     if constexpr (FORMS) {
         return shape < 2 ? tree_tiles<HD, FMT, 1, true> : shape == 2 ? tree_blocks<HD, FMT, 4, 2, 1, true> : tree_blocks<HD, FMT, 8, 1, 1, true>;
+    } else if constexpr (FMT != CF_CACHE_F16) {
+        return shape == 0 ? tree_tiles<HD, FMT, 1, false> : shape < 4 ? tree_tiles<HD, FMT, 2, false> : tree_blocks<HD, FMT, 8, 1, 2, false>;
     } else {
         static const KernelFn fn[kShapes] = {tree_tiles<HD, FMT, 1, false>, tree_tiles<HD, FMT, 2, false>, tree_blocks<HD, FMT, 4, 2, 1, false>,
                                              tree_blocks<HD, FMT, 4, 1, 2, false>, tree_blocks<HD, FMT, 8, 1, 2, false>};
@@ -952,10 +936,10 @@ Plan plan_of(const Shape (&shapes)[kShapes], int batch, int nkv, int group, int 
 {
     const int rows = tokens * group;
     Plan p;
-    for (p.shape = 0; p.shape < kShapes - 1 && rows > kPlain[p.shape].rows;) ++p.shape;
+    for (p.shape = 0; p.shape < kShapes - 1 && rows > 16 << p.shape;) ++p.shape;
     p.blocks = (rows + shapes[p.shape].rows - 1) / shapes[p.shape].rows;
     const long long items = (long long)batch * nkv * p.blocks, slots = (long long)cus * 8 / shapes[p.shape].waves;
-    const int wanted = (int)((slots + items - 1) / items), least = p.shape < 2 ? NW * kStep : 2 * kBlockStep, most = (keys + least - 1) / least;
+    const int wanted = (int)((slots + items - 1) / items), least = NW * kStep, most = (keys + least - 1) / least;
     p.splits = wanted < most ? wanted : most;
     if (p.splits > kMaxSplits) p.splits = kMaxSplits;
     if (limit > 0 && p.splits > limit) p.splits = limit;
@@ -1044,7 +1028,7 @@ int cf_tree_attend(cf_tree t, int32_t batch, const void *q, const cf_cache *cach
     a.window = t->cfg.window, a.cap = t->cfg.score_cap;
     const int keys = (a.window > 0 && a.window < draft->max_len ? a.window : draft->max_len) + draft->tokens;
     const bool forms = a.cap > 0.f || a.window > 0 || a.slopes;
-    const auto &shapes = forms ? kForms : kPlain;
+    const auto &shapes = forms ? kForms : c.format == CF_CACHE_F16 ? kPlain : kPlain8;
     Plan p = plan_of(shapes, batch, a.nkv, a.group, draft->tokens, keys, t->cus, t->max_splits);
     a.padded = p.blocks * shapes[p.shape].rows;
     const size_t rows = (size_t)batch * a.nkv * a.padded;

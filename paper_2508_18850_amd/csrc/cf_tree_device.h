@@ -36,6 +36,21 @@ __device__ __forceinline__ uint32_t pair_of_e4m3(uint32_t x, bool high)
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// Infinities and NaN among the values of a dword: the top bit of each such value, and the dword without them.
+template <int FMT>
+__device__ __forceinline__ uint32_t unfit_bits(uint32_t x)
+{
+    if constexpr (FMT == CF_CACHE_F16) return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+    if constexpr (FMT == CF_CACHE_E4M3) return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;      // (0x7f and 0xff)
+    return 0u;
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t without_unfit(uint32_t x)
+{
+    const uint32_t bad = unfit_bits<FMT>(x);
+    return x & ~(FMT == CF_CACHE_F16 ? (bad >> 15) * 0xffffu : (bad >> 7) * 0xffu);
+}
+
 // Eight codes as fp16.
 template <int FMT>
 __device__ __forceinline__ u32x4 widen(uint32_t a, uint32_t b)
@@ -79,7 +94,7 @@ struct Keys {
     }
 };
 
-// The values of a step of 32: NJ adjacent dimensions of eight rows to a lane, transposed in the lane into NJ A operands.
+// The values of a step of 32: NJ adjacent dimensions of eight rows to a lane, transposed in the lane into NJ A operands, two at a time.
 template <int HD, int FMT>
 struct Values {
     static constexpr int NJ = HD / 16, ROW = HD * cache::kValueBytes<FMT>, DW = NJ * cache::kValueBytes<FMT> / 4;     // dwords of a load: 1, 2 or 4
@@ -103,43 +118,54 @@ struct Values {
             }
         }
     }
-    __device__ __forceinline__ void operands(h8 (&f)[NJ]) const
+    // the operands of dimensions NJ c + 2 pair and NJ c + 2 pair + 1
+    __device__ __forceinline__ void operands(int pair, h8 (&f)[2]) const
     {
-        u32x4 o[NJ];
+        u32x4 o[2];
         if constexpr (FMT == CF_CACHE_F16) {
 #pragma unroll
-            for (int j2 = 0; j2 < NJ / 2; ++j2)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    o[2 * j2][w] = __builtin_amdgcn_perm(raw[2 * w + 1][j2], raw[2 * w][j2], 0x05040100u);
-                    o[2 * j2 + 1][w] = __builtin_amdgcn_perm(raw[2 * w + 1][j2], raw[2 * w][j2], 0x07060302u);
-                }
-        } else if constexpr (FMT == CF_CACHE_INT8) {
-#pragma unroll
-            for (int j4 = 0; j4 < NJ / 4; ++j4)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t lo = raw[2 * w][j4] ^ 0x80808080u, hi = raw[2 * w + 1][j4] ^ 0x80808080u;
-                    o[4 * j4][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, 0x0c040c00u));
-                    o[4 * j4 + 1][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, 0x0c050c01u));
-                    o[4 * j4 + 2][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, 0x0c060c02u));
-                    o[4 * j4 + 3][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, 0x0c070c03u));
-                }
+            for (int w = 0; w < 4; ++w) {
+                o[0][w] = __builtin_amdgcn_perm(raw[2 * w + 1][pair], raw[2 * w][pair], 0x05040100u);
+                o[1][w] = __builtin_amdgcn_perm(raw[2 * w + 1][pair], raw[2 * w][pair], 0x07060302u);
+            }
         } else {
+            const int word = pair / 2, high = pair & 1;            // two codes of a dword
 #pragma unroll
-            for (int j4 = 0; j4 < NJ / 4; ++j4)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t lo = raw[2 * w][j4], hi = raw[2 * w + 1][j4];
-                    const uint32_t a = __builtin_amdgcn_perm(hi, lo, 0x05010400u), b = __builtin_amdgcn_perm(hi, lo, 0x07030602u);
-                    o[4 * j4][w] = pair_of_e4m3(a, false);
-                    o[4 * j4 + 1][w] = pair_of_e4m3(a, true);
-                    o[4 * j4 + 2][w] = pair_of_e4m3(b, false);
-                    o[4 * j4 + 3][w] = pair_of_e4m3(b, true);
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (FMT == CF_CACHE_INT8) {
+                    const uint32_t lo = raw[2 * w][word], hi = raw[2 * w + 1][word];       // (top bits flipped: flip())
+                    o[0][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, high ? 0x0c060c02u : 0x0c040c00u));
+                    o[1][w] = pair_of_int8(__builtin_amdgcn_perm(hi, lo, high ? 0x0c070c03u : 0x0c050c01u));
+                } else {
+                    const uint32_t x = __builtin_amdgcn_perm(raw[2 * w + 1][word], raw[2 * w][word], high ? 0x07030602u : 0x05010400u);
+                    o[0][w] = pair_of_e4m3(x, false);
+                    o[1][w] = pair_of_e4m3(x, true);
                 }
+            }
         }
+        f[0] = __builtin_bit_cast(h8, o[0]), f[1] = __builtin_bit_cast(h8, o[1]);
+    }
+    // once before the operands of int8 codes
+    __device__ __forceinline__ void flip()
+    {
+        if constexpr (FMT == CF_CACHE_INT8)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) f[j] = __builtin_bit_cast(h8, o[j]);
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int w = 0; w < DW; ++w) raw[u][w] ^= 0x80808080u;
+    }
+    // Takes infinities and NaN (int8 codes have none) out; not 0 if there were some.
+    __device__ __forceinline__ uint32_t take_out_unfit()
+    {
+        uint32_t odd = 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int w = 0; w < DW; ++w) {
+                odd |= unfit_bits<FMT>(raw[u][w]);
+                raw[u][w] = without_unfit<FMT>(raw[u][w]);
+            }
+        return odd;
     }
 };
 

@@ -289,6 +289,24 @@ def test_splits_do_not_matter(fmt, T):
         assert np.array_equal(first, c.out.cpu().numpy())
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T", [1, 9, 20])
+def test_rows_of_very_different_lengths(fmt, T):
+    """One long row among short and empty ones, rows without new tokens, with a window; and many rows."""
+    _say(fmt, "lengths", T)
+    lens = [3000, 1, 0, 40, 900, 33, 0, 64, 2000, 31]
+    counts = [T, T, T, 0, T, max(T - 2, 0), 1, T, T, T]
+    for window in (0, 300):
+        c = Case(fmt, 2, 1, 64, lens, T, counts=counts, window=window, seed=26)
+        c.poison_rest()
+        first = c.check()
+        assert np.array_equal(first, c.run())
+        c.tree.set_splits(3)
+        c.check()
+    c = Case(fmt, 2, 1, 64, [(37 * b) % 600 for b in range(70)], T, counts=[T - b % 2 for b in range(70)], seed=27)
+    c.check()
+
+
 def test_long_cache():
     """Many parts with many keys each, the product of the largest shape's heads; checked on three heads."""
     for fmt, T in (("e4m3", 1), ("int8", 9), ("f16", 33)):
