@@ -931,15 +931,20 @@ KernelFn pick(int hd, int fmt, int shape, bool forms)
 constexpr int kMaxSplits = 64;
 // Partial values (fp32) that the last workgroup of a row block joins by itself.
 constexpr int kJoinedInPlace = 16384;
-// keys: the most that a row sees.  As many parts as bring eight wavefronts to a compute unit, with a step or more for every wavefront.
+// keys: the most that a row sees.  As many parts as give every compute unit a workgroup, and up to the eight wavefronts that it holds where
+// the parts then still have 1024 keys: shorter ones do not gain what joining them costs.  (64 tokens over 4096 e4m3 rows, 32 heads, 4 / 8
+// parts 17.7 / 20.6 us; one token over 32768 e4m3 rows, 8 KV heads, 32 / 64 parts 17.2 / 18.3, with 16 19.5; 32 tokens over 8192 int8 rows,
+// batch 4, 2 / 4 parts 37.6 / 32.5.)  Never fewer than 128 keys.
 Plan plan_of(const Shape (&shapes)[kShapes], int batch, int nkv, int group, int tokens, int keys, int cus, int limit)
 {
     const int rows = tokens * group;
     Plan p;
     for (p.shape = 0; p.shape < kShapes - 1 && rows > 16 << p.shape;) ++p.shape;
     p.blocks = (rows + shapes[p.shape].rows - 1) / shapes[p.shape].rows;
-    const long long items = (long long)batch * nkv * p.blocks, slots = (long long)cus * 8 / shapes[p.shape].waves;
-    const int wanted = (int)((slots + items - 1) / items), least = NW * kStep, most = (keys + least - 1) / least;
+    const long long items = (long long)batch * nkv * p.blocks;
+    const auto fill = [&](long long places) { return (int)((places + items - 1) / items); };
+    const int one = fill(cus), full = fill((long long)cus * 8 / shapes[p.shape].waves), most = (keys + NW * kStep - 1) / (NW * kStep);
+    const int wanted = keys / 1024 < one ? one : keys / 1024 < full ? keys / 1024 : full;
     p.splits = wanted < most ? wanted : most;
     if (p.splits > kMaxSplits) p.splits = kMaxSplits;
     if (limit > 0 && p.splits > limit) p.splits = limit;
