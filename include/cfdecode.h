@@ -424,9 +424,10 @@ int64_t cf_ffn_algorithmic_bytes(const cf_ffn_config *cfg, int32_t batch);
  *   CF_CACHE_F16    fp16 (the tensors that cf_decode_block and cf_decode_layer take; no scales)
  *   CF_CACHE_E4M3   8-bit floats (OCP e4m3: 448 is the largest) and one fp32 scale for every cached row of a head,
  *   CF_CACHE_INT8   8-bit integers (-127..127)                  scales [batch, n_kv_heads, max_seq]; a value is code * scale
- * (at least 0; what these calls write is).  A row (head_dim fp16 values) is held in 8 bits as  scale = top / Q  and  code = x * Q / top  rounded to the nearest code, ties
- * to even, where top is the row's largest magnitude and Q = 448 or 127; the code is the correctly rounded one.  A row of zeros has
+ * A row (head_dim fp16 values) is held in 8 bits as  scale = top / Q  and  code = x * Q / top  rounded to the nearest code, ties to
+ * even, where top is the row's largest magnitude and Q = 448 or 127; the code is the correctly rounded one.  A row of zeros has
  * scale 0 and codes 0; a row that holds an infinity or a NaN has scale NaN and codes 0, so that all of it reads back as NaN.
+ * (Scales that another program writes have to be at least 0 as well, or NaN.)
  */
 enum { CF_CACHE_F16 = 0, CF_CACHE_E4M3 = 1, CF_CACHE_INT8 = 2 };
 typedef struct cf_cache_config {
@@ -470,15 +471,16 @@ typedef struct cf_draft {
  * cf_cache_append: qkv [batch, tokens, (n_q + 2 n_kv) * head_dim] fp16, columns ordered as those of W_qkv in cf_decode_block (the
  *   product of the tokens' hidden states with it); queries and keys are rotated for their positions as in cf_decode_block (angles
  *   and products in fp64, one rounding to fp16), q_out [batch, tokens, n_q, head_dim] fp16 receives the queries, the cache rows
- *   row_len[b] + t the keys and values.  Any number of tokens that the cache holds: a prompt, a tree, one token.  q_out must not
- *   overlap qkv.
+ *   row_len[b] + t the keys and values.  Any number of tokens that the cache holds: a prompt, a tree, one token.  qkv, q_out and
+ *   the cache must not overlap each other.
  * cf_cache_read: rows first .. first + rows - 1 of every head's slice as fp16, k_out and v_out [batch, n_kv, rows, head_dim]; 8-bit
- *   values are rounded once more, from the fp32 product code * scale.  rows 0 does nothing.
+ *   values are rounded once more, from the fp32 product code * scale.  rows 0 does nothing.  k_out, v_out and the cache must not
+ *   overlap each other.
  * cf_cache_keep: after verification, row row_len[b] + i of every head's slice becomes what row row_len[b] + kept[b][i] was, for
  *   i < n_kept[b] (keys, values and scales; all rows are read before one is written); the rows behind stay as they were.  kept: DEVICE [batch,
  *   tokens] int32, entries clamped into 0..n_b - 1; they may come in any order and more than once; n_kept: DEVICE [batch] int32,
- *   clamped into 0..n_b.  new_len: DEVICE [batch] int32 that receives row_len[b] + n_kept[b], or NULL; it must not overlap the
- *   other arrays.  draft's depth, tree and per_row are not looked at; tokens at most 256 (CF_EUNSUPPORTED).
+ *   clamped into 0..n_b.  new_len: DEVICE [batch] int32 that receives row_len[b] + n_kept[b], or NULL; it must not overlap
+ *   another array.  draft's depth, tree and per_row are not looked at; tokens at most 256 (CF_EUNSUPPORTED).
  */
 int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, const cf_cache *cache, const cf_draft *draft,
                     void *q_out, void *stream);
@@ -495,15 +497,16 @@ int cf_cache_keep(const cf_cache_config *cfg, int32_t batch, const cf_cache *cac
  *   out = sum_j softmax(s)_j v_j
  *
  * q [batch, tokens, n_q, head_dim] fp16, rotated (q_out of cf_cache_append); the drafted tokens' keys and values are in the cache
- * already; the position of cached row j is j, that of a drafted token as above.  slopes: DEVICE [n_q] fp32, finite, 4-byte aligned, or NULL.
- * out [batch, tokens, n_q, head_dim] fp16, must not overlap q: rows of padding stay as they were; a token that sees no key, or
- * only keys with a score of minus infinity, gets zeros.  What a token does not see does not enter its result, whatever it holds
- * (NaN and infinities among it).  Scores, softmax statistics and sums are fp32.  With the same row_len, row_tokens, max_len and batch the same
- * inputs give the same bits; otherwise the last bits may depend on how the cached rows are divided.
+ * already; the position of cached row j is j, that of a drafted token as above (for the bias and the window taken to within
+ * -2^30 .. 2^30).  slopes: DEVICE [n_q] fp32, 4-byte aligned, or NULL; their size times a distance must stay below 1e29.
+ * out [batch, tokens, n_q, head_dim] fp16, must not overlap q or the cache: rows of padding stay as they were; a token that sees
+ * no key, or only keys with a score of minus infinity, gets zeros.  What a token does not see does not enter its result, whatever
+ * it holds (NaN and infinities among it).  Scores, softmax statistics and sums are fp32.  With the same row_len, row_tokens, max_len
+ * and batch the same inputs give the same bits; otherwise the last bits may depend on how the cached rows are divided.
  *
  * cf_tree_create: a handle on the current device for calls of up to max_tokens tokens (1..256) with this score_cap (0: none) and
  *   window (0: none).  Allocates a workspace for partial results (synchronous).  CF_EINVAL also for a negative or non-finite
- *   score_cap and a negative window.  A handle must not be used from two streams at the same time, nor two captured graphs with
+ *   score_cap and a negative window, CF_EUNSUPPORTED for a score_cap that is neither 0 nor in 2^-60 .. 2^60.  A handle must not be used from two streams at the same time, nor two captured graphs with
  *   calls on one handle replayed at the same time, and only while its device is the current one (CF_EINVAL).
  * cf_tree_set_splits: upper limit on the number of parts a sequence's keys are divided into; 0 = chosen by the library.  For
  *   tests and measurements; CF_EINVAL outside 0..64.

@@ -238,7 +238,10 @@ int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, 
     if (rc != CF_OK) return rc;
     if (!qkv || !q_out || !aligned(qkv, 16) || !aligned(q_out, 16)) return CF_EINVAL;
     const size_t head_values = (size_t)batch * draft->tokens * cfg->head_dim;
-    if (overlap(qkv, 2 * head_values * (cfg->n_q_heads + 2 * (size_t)cfg->n_kv_heads), q_out, 2 * head_values * cfg->n_q_heads)) return CF_EINVAL;
+    const size_t qkv_bytes = 2 * head_values * (cfg->n_q_heads + 2 * (size_t)cfg->n_kv_heads), q_bytes = 2 * head_values * cfg->n_q_heads;
+    if (overlap(qkv, qkv_bytes, q_out, q_bytes) || in_cache(*cfg, *cache, batch, qkv, qkv_bytes) ||
+        in_cache(*cfg, *cache, batch, q_out, q_bytes) || tangled(*cfg, *cache, batch))
+        return CF_EINVAL;
     AppendArgs a;
     std::memset(&a, 0, sizeof a);
     a.qkv = static_cast<const uint16_t *>(qkv);
@@ -268,6 +271,10 @@ int cf_cache_read(const cf_cache_config *cfg, int32_t batch, const cf_cache *cac
     if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16) || first < 0 || rows < 0 || (long long)first + rows > cfg->max_seq)
         return CF_EINVAL;
     if (rows == 0) return CF_OK;
+    const size_t out_bytes = 2 * (size_t)batch * cfg->n_kv_heads * rows * cfg->head_dim;
+    if (overlap(k_out, out_bytes, v_out, out_bytes) || in_cache(*cfg, *cache, batch, k_out, out_bytes) ||
+        in_cache(*cfg, *cache, batch, v_out, out_bytes))
+        return CF_EINVAL;
     ReadArgs a;
     std::memset(&a, 0, sizeof a);
     a.k = static_cast<const char *>(cache->k), a.v = static_cast<const char *>(cache->v);
@@ -289,7 +296,12 @@ int cf_cache_keep(const cf_cache_config *cfg, int32_t batch, const cf_cache *cac
     if (rc == CF_OK) rc = check_draft(*cfg, draft);
     if (rc != CF_OK) return rc;
     if (!kept || !n_kept || !aligned(kept, 4) || !aligned(n_kept, 4) || !aligned(new_len, 4)) return CF_EINVAL;
-    if (new_len && (new_len == draft->row_len || new_len == draft->row_tokens || new_len == n_kept || new_len == kept)) return CF_EINVAL;
+    const size_t a_row = 4 * (size_t)batch;                         // bytes of an int32 for every batch row
+    if (new_len && ((draft->row_len && overlap(new_len, a_row, draft->row_len, a_row)) ||
+                    (draft->row_tokens && overlap(new_len, a_row, draft->row_tokens, a_row)) || overlap(new_len, a_row, n_kept, a_row) ||
+                    overlap(new_len, a_row, kept, a_row * draft->tokens) || in_cache(*cfg, *cache, batch, new_len, a_row)))
+        return CF_EINVAL;
+    if (tangled(*cfg, *cache, batch)) return CF_EINVAL;
     if (draft->tokens > kMaxKept) return CF_EUNSUPPORTED;
     KeepArgs a;
     std::memset(&a, 0, sizeof a);

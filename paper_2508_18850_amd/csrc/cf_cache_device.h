@@ -56,6 +56,22 @@ inline int check_cache(const cf_cache_config &c, const cf_cache *p, int32_t batc
     if ((long long)batch * c.n_kv_heads > 65535) return CF_EUNSUPPORTED;      // second dimension of the grids
     return CF_OK;
 }
+// Whether [x, x + bytes) shares memory with a cache of `batch` rows; whether the cache's own buffers do with each other.
+inline size_t cached_rows(const cf_cache_config &c, int32_t batch) { return (size_t)batch * c.n_kv_heads * c.max_seq; }
+inline size_t buffer_bytes(const cf_cache_config &c, int32_t batch) { return cached_rows(c, batch) * c.head_dim * (c.format == CF_CACHE_F16 ? 2 : 1); }
+inline bool in_cache(const cf_cache_config &c, const cf_cache &p, int32_t batch, const void *x, size_t bytes)
+{
+    const size_t rows = buffer_bytes(c, batch), scales = 4 * cached_rows(c, batch);
+    if (overlap(x, bytes, p.k, rows) || overlap(x, bytes, p.v, rows)) return true;
+    return c.format != CF_CACHE_F16 && (overlap(x, bytes, p.k_scale, scales) || overlap(x, bytes, p.v_scale, scales));
+}
+inline bool tangled(const cf_cache_config &c, const cf_cache &p, int32_t batch)
+{
+    const size_t rows = buffer_bytes(c, batch), scales = 4 * cached_rows(c, batch);
+    if (overlap(p.k, rows, p.v, rows)) return true;
+    return c.format != CF_CACHE_F16 && (overlap(p.k_scale, scales, p.v_scale, scales) || overlap(p.k_scale, scales, p.k, rows) ||
+                                        overlap(p.k_scale, scales, p.v, rows) || overlap(p.v_scale, scales, p.k, rows) || overlap(p.v_scale, scales, p.v, rows));
+}
 inline int check_draft(const cf_cache_config &c, const cf_draft *d)
 {
     if (!d || d->tokens < 1 || d->max_len < 0 || (long long)d->max_len + d->tokens > c.max_seq) return CF_EINVAL;

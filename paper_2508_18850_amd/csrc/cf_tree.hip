@@ -144,6 +144,16 @@ __device__ __forceinline__ float score_factor(float cap)
     return cap > 0.f ? unit * 2.f / cap : unit;                    // with a cap: twice its share of the cap, for the tanh
 }
 
+// tanh(y) for x = 2 y log2(e): 1 - 2 / (2^x + 1), which is off by 2^-23 of one, and for |x| < 1/2, where that would be much of the result,
+// the odd series of tanh up to the seventh power (the ninth is less than 2^-25 of it).
+__device__ __forceinline__ float tanh_(float x)
+{
+    constexpr float h = 0.34657359027997265f, h2 = h * h;           // y = h x
+    const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(exp2_(x) + 1.f), z = x * x * h2;
+    const float near = x * h * fmaf(fmaf(fmaf(-17.f / 315.f, z, 2.f / 15.f), z, -1.f / 3.f), z, 1.f);
+    return fabsf(x) < 0.5f ? near : far;
+}
+
 // Arguments x_j of a row for two tiles of 16 keys from j0 on; minus infinity for a key that it does not see.
 template <int FMT, bool FORMS>
 __device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row &row, int g, int j0, bool masked, float to_score,
@@ -163,7 +173,7 @@ __device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq,
                 key_at = j >= sq.len ? theirs : j;
             }
             const int distance = row.at - key_at;
-            if (a.cap > 0.f) x[e] = a.cap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(exp2_(x[e]) + 1.f));      // tanh
+            if (a.cap > 0.f) x[e] = a.cap * kLog2e * tanh_(x[e]);
             x[e] -= row.slope * (float)distance;
             if (masked && a.window > 0) seen = seen && distance < a.window;
         }
@@ -299,8 +309,8 @@ struct Part {
         int lo = 0;
         all_from = 0;
         if (FORMS && a.window > 0) {
-            lo = min(max(__builtin_amdgcn_readfirstlane(nearest) - a.window + 1, 0), sq.len);
-            all_from = max(__builtin_amdgcn_readfirstlane(farthest) - a.window + 1, 0);
+            lo = min(max(__builtin_elementwise_sub_sat(__builtin_amdgcn_readfirstlane(nearest), a.window) + 1, 0), sq.len);
+            all_from = max(__builtin_elementwise_sub_sat(__builtin_amdgcn_readfirstlane(farthest), a.window) + 1, 0);
         }
         const int first = lo / STEP, steps = (sq.end + STEP - 1) / STEP - first, per = (steps + a.splits - 1) / a.splits;
         begin = first + at.split * per, end = min(first + steps, begin + per);
@@ -972,6 +982,7 @@ int cf_tree_create(const cf_tree_config *cfg, cf_tree *out)
     const int rc = check_config(cfg->cache);
     if (rc != CF_OK) return rc;
     if (cfg->max_tokens < 1 || cfg->max_tokens > kMaxTokens || cfg->window < 0 || !(cfg->score_cap >= 0.f) || !(cfg->score_cap <= 3.402823466e38f)) return CF_EINVAL;
+    if (cfg->score_cap > 0.f && (cfg->score_cap < 0x1p-60f || cfg->score_cap > 0x1p60f)) return CF_EUNSUPPORTED;   // 2 / cap and cap log2 e in fp32
     int dev = 0, cus = 0;
     if (hipGetDevice(&dev) != hipSuccess ||
         hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
@@ -1015,7 +1026,7 @@ int cf_tree_attend(cf_tree t, int32_t batch, const void *q, const cf_cache *cach
     if (rc != CF_OK) return rc;
     if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !aligned(slopes, 4) || draft->tokens > t->cfg.max_tokens) return CF_EINVAL;
     const size_t q_bytes = 2 * (size_t)batch * draft->tokens * c.n_q_heads * c.head_dim;
-    if (overlap(q, q_bytes, out, q_bytes)) return CF_EINVAL;
+    if (overlap(q, q_bytes, out, q_bytes) || in_cache(c, *cache, batch, out, q_bytes)) return CF_EINVAL;
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return CF_EHIP;
     if (dev != t->device) return CF_EINVAL;

@@ -157,6 +157,25 @@ def test_forms_of_the_score(fmt, cap, window, slopes):
     Case(fmt, 8, 1, 128, [0, 65], 4, counts=[4, 2], cap=cap, window=window, slopes=slopes, seed=8).check()
 
 
+# a cap far above the scores, where 1 - 2 / (2^x + 1) alone would leave little of them, near them, and far below (the mean of the values)
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("cap", [2.0 ** -60, 1e-3, 2.5, 300.0, 1e5, 1e9, 2.0 ** 60])
+def test_caps_of_any_size(fmt, cap):
+    _say(fmt, "cap", cap)
+    Case(fmt, 4, 2, 64, [190, 23], 6, cap=cap, seed=31, q_size=3.0).check()
+    Case(fmt, 4, 1, 128, [200], 40, cap=cap, seed=32, q_size=3.0).check()
+
+
+@pytest.mark.parametrize("T", [3, 80])
+def test_positions_before_the_first_and_any_window(T):
+    """Depths that lead before row 0, and windows up to the largest: nothing is lost to an overflow."""
+    for window in (1, 50, 2 ** 31 - 1):
+        for lowest in (-100, -2 ** 30 + 1000):
+            _say("T", T, "window", window, "lowest", lowest)
+            base = Case("f16", 4, 2, 64, [70, 5], T, window=window, seed=33)
+            Case("f16", 4, 2, 64, [70, 5], T, window=window, seed=33, depth=base.depth + lowest).check()
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_chain_needs_no_masks(fmt):
     c = Case(fmt, 4, 2, 64, [50, 20], 20, chain=True, seed=9)
@@ -395,6 +414,9 @@ def test_refusals():
     for n in (-1, 65):
         with pytest.raises(lib.CfError):
             tree.set_splits(n)
+    apart = lib.cache_pointers(p + 8192, p + 16384, p + 32768, p + 40960)      # rows of 2 heads x 100 x 64 codes: 12800 bytes
+    for out in (p + 8192, p + 16384 + 12800 - 16, p + 32768, p + 40960 + 784):
+        assert bad(tree.attend_rc(1, p, apart, ok, 0, out))
     torch.cuda.synchronize()
 
 

@@ -194,3 +194,25 @@ def test_algorithmic_bytes():
     assert raw.cf_tree_algorithmic_bytes(ctypes.byref(cfg), 2, 3, 40) == 2 * (2 * 4 * 128 * 43 + 4 * 3 * 8 * 64)
     cfg = lib.TreeConfig(_kv(format=2).cfg, 8, 0.0, 10)
     assert raw.cf_tree_algorithmic_bytes(ctypes.byref(cfg), 1, 3, 40) == 2 * 4 * 68 * 13 + 4 * 3 * 8 * 64
+
+
+def test_buffers_that_overlap_are_refused():
+    import ctypes
+    import paper_2508_18850_amd as lib
+    kv, c, d = _kv(), _pointers(), _draft()                         # of a batch of 1: 25600 bytes of keys, 1600 of their scales
+    end, far = P + 25600, 8 * P
+    for where in (P, end - 16, 2 * P, 3 * P, 3 * P + 1600 - 16, 4 * P):
+        assert kv.append_rc(1, where, c, d, far) == EINVAL and kv.append_rc(1, far, c, d, where) == EINVAL
+        assert kv.read_rc(1, c, 0, 1, where, far) == EINVAL and kv.read_rc(1, c, 0, 1, far, where) == EINVAL
+        assert kv.keep_rc(1, c, d, far, far + 64, where) == EINVAL
+    assert kv.read_rc(1, c, 0, 2, far, far + 1008) == EINVAL        # 4 heads x 2 rows x 64 fp16 values: 1024 bytes
+    for over in (dict(v=end - 16), dict(k_scale=end - 16), dict(v_scale=2 * P), dict(v_scale=3 * P + 1596)):
+        assert kv.append_rc(1, far, _pointers(**over), d, 9 * P) == EINVAL
+        assert kv.keep_rc(1, _pointers(**over), d, far, far + 64) == EINVAL
+    two = _draft(row_len=far + 256)
+    for new_len in (far + 252, far + 260, far + 28, far + 68):      # of a batch of 2: on row_len, on kept [2][4], on n_kept
+        assert kv.keep_rc(2, c, two, far, far + 64, new_len) == EINVAL
+    h = ctypes.c_void_p()
+    for cap in (1e-19, 1.2e18):
+        cfg = lib.TreeConfig(kv.cfg, 4, cap, 0)
+        assert lib.load_library().cf_tree_create(ctypes.byref(cfg), ctypes.byref(h)) == EUNSUPPORTED and not h
