@@ -17,6 +17,7 @@
 #include "cf_lanes_device.h"
 #include "cf_tree_device.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -905,6 +906,7 @@ using KernelFn = void (*)(const TreeArgs);
 struct Plan {
     int shape;                     // index into kShapes
     int blocks, splits;
+    bool in_place;                 // the last workgroup of a row block joins its parts
 };
 // Rows of a workgroup: tree_tiles with one or two tiles of 16, tree_blocks with two groups of four wavefronts of one tile, four of two, or
 // eight of two.  With forms of the score one tile to a wavefront (more do not fit the registers).
@@ -913,6 +915,11 @@ struct Shape {
     int rows, waves;
 };
 constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 8}, {128, 4}, {256, 8}}, kPlain8[kShapes] = {{16, 4}, {32, 4}, {32, 4}, {32, 4}, {256, 8}}, kForms[kShapes] = {{16, 4}, {16, 4}, {64, 8}, {128, 8}, {128, 8}};
+
+const Shape (&shapes_of(const cf_cache_config &c, bool forms))[kShapes]
+{
+    return forms ? kForms : c.format == CF_CACHE_F16 ? kPlain : kPlain8;
+}
 
 template <int HD, int FMT, bool FORMS>
 KernelFn pick_shape(int shape)
@@ -939,26 +946,45 @@ KernelFn pick(int hd, int fmt, int shape, bool forms)
 }
 
 constexpr int kMaxSplits = 64;
-// Partial values (fp32) that the last workgroup of a row block joins by itself.
-constexpr int kJoinedInPlace = 16384;
-// keys: the most that a row sees.  As many parts as give every compute unit a workgroup, and up to the eight wavefronts that it holds where
-// the parts then still have 1024 keys: shorter ones do not gain what joining them costs.  (64 tokens over 4096 e4m3 rows, 32 heads, 4 / 8
-// parts 17.7 / 20.6 us; one token over 32768 e4m3 rows, 8 KV heads, 32 / 64 parts 17.2 / 18.3, with 16 19.5; 32 tokens over 8192 int8 rows,
-// batch 4, 2 / 4 parts 37.6 / 32.5.)  Never fewer than 128 keys.
-Plan plan_of(const Shape (&shapes)[kShapes], int batch, int nkv, int group, int tokens, int keys, int cus, int limit)
+// Parts that the last workgroup of a row block joins by itself have at most this many values (fp32) together, where there are many row
+// blocks, whose join kernel would read as much again, the second number.  (Against the join kernel: up to 4096 values -0.7 us, 8192 to 10240
+// -0.3, 12288 to 16384 +0.3 with 8 row blocks, 0 with 32, -0.5 with 48, -0.7 with 64; 32768 +12.)
+constexpr int kJoinedInPlace = 10240, kManyInPlace = 16384, kManyBlocks = 32;
+
+// keys: the most that a row sees.  A part costs time in proportion to its keys and, where they are joined in place, to its being one more,
+// so that the best number of parts grows with the root of the keys: sqrt(keys / 24) for plain scores.  (One token, 8 KV heads, int8, 8 / 16 / 32
+// parts: 2048 rows 8.7 / 8.9 / 9.7 us, 8192 rows 13.1 / 11.3 / 12.3.)  The join kernel costs about the same for any number: three times as
+// many keys under the root.  (One token, 64 heads, fp16, 4096 rows: 12 / 16 / 24 / 32 parts 11.7 / 11.5 / 10.6 / 10.5.)  Scores with forms take
+// twice the time per key.  No more than give every compute unit a workgroup, or, where parts then still have 1024 keys, the eight
+// wavefronts that it holds (32 tokens over 8192 int8 rows, batch 4, 2 / 4 parts 37.6 / 32.5 us; 64 tokens over 4096 e4m3 rows, 32 heads, 4 / 8
+// parts 17.7 / 20.6).  Never fewer than 128 keys, and one part up to 384 keys where a workgroup has at most 64 rows: nothing to join
+// saves 0.7 to 1.7 us.  Parts are whole multiples of 128 keys, so that all wavefronts have as many steps.
+Plan plan_of(const cf_cache_config &c, bool forms, int batch, int tokens, int keys, int cus, int limit)
 {
-    const int rows = tokens * group;
+    const auto &shapes = shapes_of(c, forms);
+    const int live = tokens * (c.n_q_heads / c.n_kv_heads);
     Plan p;
-    for (p.shape = 0; p.shape < kShapes - 1 && rows > 16 << p.shape;) ++p.shape;
-    p.blocks = (rows + shapes[p.shape].rows - 1) / shapes[p.shape].rows;
-    const long long items = (long long)batch * nkv * p.blocks;
+    for (p.shape = 0; p.shape < kShapes - 1 && live > 16 << p.shape;) ++p.shape;
+    const Shape &shape = shapes[p.shape];
+    p.blocks = (live + shape.rows - 1) / shape.rows;
+    const long long items = (long long)batch * c.n_kv_heads * p.blocks;
     const auto fill = [&](long long places) { return (int)((places + items - 1) / items); };
-    const int one = fill(cus), full = fill((long long)cus * 8 / shapes[p.shape].waves), most = (keys + NW * kStep - 1) / (NW * kStep);
-    const int wanted = keys / 1024 < one ? one : keys / 1024 < full ? keys / 1024 : full;
-    p.splits = wanted < most ? wanted : most;
+    const auto in_place = [&](int parts) {
+        const long long values = (long long)parts * (live < shape.rows ? live : shape.rows) * c.head_dim;
+        return values <= kJoinedInPlace || (values <= kManyInPlace && items >= kManyBlocks);
+    };
+    const int one = fill(cus), full = fill((long long)cus * 8 / shape.waves), most = (keys + 4 * kStep - 1) / (4 * kStep);
+    // parts of as many times 128 keys
+    const auto in_rounds = [&](double rounds) { return std::min((int)std::ceil(most / std::max(std::floor(rounds), 1.0)), one); };
+    const double work = forms ? 2.0 * keys : keys;
+    int few = in_rounds(most / std::sqrt(work / 24) + 0.5);
+    if (!in_place(few)) few = in_rounds(most / std::sqrt(work / 8));
+    const int wanted = keys / 1024 < few ? few : keys / 1024 < full ? keys / 1024 : full;
+    p.splits = keys <= 384 && shape.rows <= 64 ? 1 : std::min(wanted, most);
     if (p.splits > kMaxSplits) p.splits = kMaxSplits;
-    if (limit > 0 && p.splits > limit) p.splits = limit;
+    if (limit > 0) p.splits = p.splits > limit ? limit : p.splits;
     if (p.splits < 1) p.splits = 1;
+    p.in_place = in_place(p.splits);
     return p;
 }
 
@@ -1044,27 +1070,25 @@ int cf_tree_attend(cf_tree t, int32_t batch, const void *q, const cf_cache *cach
     a.window = t->cfg.window, a.cap = t->cfg.score_cap;
     const int keys = (a.window > 0 && a.window < draft->max_len ? a.window : draft->max_len) + draft->tokens;
     const bool forms = a.cap > 0.f || a.window > 0 || a.slopes;
-    const auto &shapes = forms ? kForms : c.format == CF_CACHE_F16 ? kPlain : kPlain8;
-    Plan p = plan_of(shapes, batch, a.nkv, a.group, draft->tokens, keys, t->cus, t->max_splits);
-    a.padded = p.blocks * shapes[p.shape].rows;
+    Plan p = plan_of(c, forms, batch, draft->tokens, keys, t->cus, t->max_splits);
+    const Shape shape = shapes_of(c, forms)[p.shape];
+    a.padded = p.blocks * shape.rows;
     const size_t rows = (size_t)batch * a.nkv * a.padded;
     if (rows * p.splits > t->ws_rows) p.splits = rows < t->ws_rows ? (int)(t->ws_rows / rows) : 1;
     a.splits = p.splits, a.blocks = p.blocks, a.units = batch * a.nkv * p.splits;
     const size_t sums = t->ws_rows * c.head_dim * sizeof(float);
     a.part = reinterpret_cast<float *>(t->ws + t->counters * sizeof(uint32_t));
     a.part_ml = (uint32_t)sums, a.part_bytes = (uint32_t)(sums + t->ws_rows * sizeof(float2));
-    const int live = draft->tokens * a.group, block_rows = live < shapes[p.shape].rows ? live : shapes[p.shape].rows;
-    if (p.splits * block_rows * c.head_dim <= kJoinedInPlace && (uint32_t)batch * a.nkv * p.blocks <= t->counters)
-        a.arrived = reinterpret_cast<uint32_t *>(t->ws);
+    if (p.in_place && (uint32_t)batch * a.nkv * p.blocks <= t->counters) a.arrived = reinterpret_cast<uint32_t *>(t->ws);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(pick(c.head_dim, c.format, p.shape, forms), dim3((a.units + 7) / 8 * 8 * p.blocks),
-                       dim3(64 * shapes[p.shape].waves), 0, s, a);
+                       dim3(64 * shape.waves), 0, s, a);
     if (hipGetLastError() != hipSuccess) return CF_EHIP;
     if (p.splits > 1 && !a.arrived) {
         const int slots = NT / (c.head_dim / 8);
         int lanes = 1;
         while (lanes < p.splits && lanes < slots) lanes *= 2;
-        hipLaunchKernelGGL((c.head_dim == 64 ? tree_join<64> : tree_join<128>), dim3((live * lanes + slots - 1) / slots, batch * a.nkv), dim3(NT), 0, s, a,
+        hipLaunchKernelGGL((c.head_dim == 64 ? tree_join<64> : tree_join<128>), dim3((draft->tokens * a.group * lanes + slots - 1) / slots, batch * a.nkv), dim3(NT), 0, s, a,
                            lanes, c.format == CF_CACHE_INT8 ? cf::tree::kInt8Unit : 1.f);
         if (hipGetLastError() != hipSuccess) return CF_EHIP;
     }
