@@ -23,7 +23,9 @@ constexpr int kMaxKept = 256;      // tokens of a cf_cache_keep: their rows are 
 // and handed to all heads through LDS.
 // Arithmetic: angle, cos, sin and the rotation are fp64 and the result is rounded to fp16 once.  A fp32 rotation is off by 2^-23, which
 // moves one value in some thousands to the other fp16 neighbour, and through it one 8-bit code in 10^5; the fp64 one gives the
-// definition's bits.
+// definition's bits; the vector units are idle beside it all the same (27.6 million instructions of 16384 wavefronts in 70 us).
+// Bound: memory.  Two prompts of 8192 and 4096 tokens, 32 + 2 x 8 heads of 128 dimensions, into int8: 324 MB in 70 us, 4.6 TB/s (a copy
+// reaches 4.8).  With few tokens the launch: one token 3.6 us on the GPU, so its heads are spread over more workgroups.
 struct AppendArgs {
     const uint16_t *qkv;
     uint16_t *q_out;
@@ -116,6 +118,9 @@ __global__ __launch_bounds__(NT) void cache_append(const AppendArgs a)
 
 // ---- read ------------------------------------------------------------------------------------------------------------------
 
+// Sixteen codes of a row and its scale to a thread, 32 bytes out; 8-bit codes are turned into fp32 by the conversion instructions, the product
+// with the scale is rounded to fp16 once.  Bound: memory.  16 x 3511 rows, 8 heads of 128 dimensions, e4m3: 349 MB in 75.7 us, 4.6 TB/s
+// (a copy reaches 4.8); a small one 3.7 us, the launch.
 struct ReadArgs {
     const char *k, *v;
     const float *k_scale, *v_scale;
@@ -183,6 +188,7 @@ struct KeepArgs {
 };
 
 // One workgroup per head's slice: its kept rows into LDS, a barrier, and out to their places (a place may be another row's source).
+// Bound: the launch and one trip to memory and back, 2.8 us for up to 128 slices; a call 6.8 us, which is the host's part.
 __global__ __launch_bounds__(NT) void cache_keep(const KeepArgs a)
 {
     extern __shared__ char held[];

@@ -2,16 +2,16 @@
 //
 // The rows of one KV head's queries (token t, query head hh of the group: row t * group + hh) are cut into blocks, the keys of a sequence
 // into parts; a workgroup takes one block over one part.  Scores and weighted values are matrix products (cf_tree_device.h).  Two
-// kernels: up to 32 rows the four wavefronts of a workgroup take steps of 32 keys in turn, each with all rows, and keys and values go from
-// memory into registers as the operands want them (tree_tiles); with more rows the wavefronts divide the rows and share steps of 64 keys,
-// which are staged in LDS as fp16 (tree_blocks), so that 8-bit codes are converted once for all rows.
+// kernels: with blocks of up to 32 rows the four wavefronts of a workgroup take steps of 32 keys in turn, each with all rows, and keys and
+// values go from memory into registers as the operands want them (tree_tiles); with larger ones the wavefronts divide the rows and share
+// steps of 64 keys, which are staged in LDS as fp16 (tree_blocks), so that 8-bit codes are converted once for all rows.
 //
 // Softmax in one pass.  Every row keeps a reference mm, the sum l of 2^(x_j - mm) and the sums of w_j v_j with
 // w_j = 2^(x_j - mm) * scale_j (x_j: score in units of log2 e, scale_j: scale of an 8-bit value row, else 1), so that values enter the
 // product as codes.  mm is moved, and what has been summed brought to the new one, only when some w_j exceeds 2^15: to where the
 // largest w_j that the row has seen is 2^7.  w_j is rounded to fp16 for the product (half a step, 2^-11 of each weight: about as much as
-// the rounding of the result; below 2^-14, that is 2^-21 of the largest, half of 2^-24); all else is fp32.  Each row's own scores alone decide when its mm moves, so
-// that what it does not see leaves its bits alone.
+// the rounding of the result; below 2^-14, that is 2^-21 of the largest, half of 2^-24); all else is fp32.  Each row's own scores alone
+// decide when its mm moves, so that what it does not see leaves its bits alone.
 #include "../../include/cfdecode.h"
 #include "cf_cache_device.h"
 #include "cf_lanes_device.h"
@@ -496,6 +496,11 @@ __device__ __forceinline__ int join_lanes(int splits, int rows, int slots)
     return lanes;
 }
 
+// Few rows: reading the keys and values is the work.  Every wavefront has its own steps, so that no barrier holds up its loads: the next step's
+// keys are requested as soon as this one's are used, and its values.  The four wavefronts' sums are joined once, through LDS.
+// Bound: memory where the cache is long (one token over 32768 e4m3 rows, 64 heads: 69 MB in 14.2 us, 4.9 TB/s, then the join; a copy
+// reaches 4.8), the chain launch - lengths - queries - keys - values - sums where it is short (256 rows 5.7 us from launch to launch).
+// Eight wavefronts to a workgroup were 5 % slower over 117 shapes: they start later and have more to join.
 // FORMS: the scores may be capped, biased or windowed.
 template <int HD, int FMT, int NR, bool FORMS>
 __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
@@ -686,6 +691,11 @@ __device__ __forceinline__ h8 transposed(const char *v, int first, int dim, int 
 // RW wavefronts with 16 NR rows each share the steps of a part; with KG = 2 there are two such groups, one for each half of a step, whose
 // sums are joined at the end.  (One group needs 1.15 us for a step of 128 dimensions when it has the compute unit for itself, most of it
 // the time from one instruction to the next that needs its result.)
+// Bound with many rows: the vector units.  Of the 2190 cycles that a wavefront with 32 rows takes for half a step (32 int8 keys, 128
+// dimensions), 590 are the scores' products, 1090 the weights (an exponential costs 8 cycles, and everything else of a weight as much
+// again), 510 the values' products; two such wavefronts share a SIMD and overlap in part.  16 x 64 tokens over 8192 int8 rows, 32 heads:
+// 138 GFLOP in 167 us, 0.83 PFLOP/s (a large fp16 product reaches 1.24), the matrix units busy a third of the time.
+// Two groups in antiphase, steps of 128 keys and requests two steps ahead were 0 to 15 % slower.
 template <int HD, int FMT, int RW, int KG, int NR, bool FORMS>
 __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 {
@@ -891,7 +901,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     }
 }
 
-// The parts of a sequence joined by a kernel of its own: as many rows to a workgroup as its threads have.
+// The parts of a sequence joined by a kernel of its own: as many rows to a workgroup as its threads have.  Bound: memory, behind a launch
+// (64 rows of 32 heads in 8 parts, 8 MB, 4.8 us; 256 rows of 128 heads in 2 parts, 34 MB, 9.4 us, 3.6 TB/s).
 template <int HD>
 __global__ __launch_bounds__(NT) void tree_join(const TreeArgs a, int lanes, float unit_v)
 {
@@ -909,12 +920,17 @@ struct Plan {
     bool in_place;                 // the last workgroup of a row block joins its parts
 };
 // Rows of a workgroup: tree_tiles with one or two tiles of 16, tree_blocks with two groups of four wavefronts of one tile, four of two, or
-// eight of two.  With forms of the score one tile to a wavefront (more do not fit the registers).
+// eight of two.  (fp16, 33 to 64 rows in two groups against one: 16 tokens over 8192 rows, batch 4 30.1 / 33.6 us.)  8-bit caches up to
+// 128 rows take blocks of 32 rows, which read the codes several times, out of the die's L2 but for the first: 64 tokens over 4096 e4m3
+// rows 20.3 / 22.1 us, 32 tokens over 8192 int8 rows, batch 4 32.8 / 37.0.  With forms of the score one tile to a wavefront (more do not
+// fit the registers).
 constexpr int kShapes = 5;
 struct Shape {
     int rows, waves;
 };
-constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 8}, {128, 4}, {256, 8}}, kPlain8[kShapes] = {{16, 4}, {32, 4}, {32, 4}, {32, 4}, {256, 8}}, kForms[kShapes] = {{16, 4}, {16, 4}, {64, 8}, {128, 8}, {128, 8}};
+constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 8}, {128, 4}, {256, 8}};
+constexpr Shape kPlain8[kShapes] = {{16, 4}, {32, 4}, {32, 4}, {32, 4}, {256, 8}};
+constexpr Shape kForms[kShapes] = {{16, 4}, {16, 4}, {64, 8}, {128, 8}, {128, 8}};
 
 const Shape (&shapes_of(const cf_cache_config &c, bool forms))[kShapes]
 {
