@@ -24,7 +24,7 @@ constexpr int kMaxKept = 256;      // tokens of a cf_cache_keep: their rows are 
 // Arithmetic: angle, cos, sin and the rotation are fp64 and the result is rounded to fp16 once.  A fp32 rotation is off by 2^-23, which
 // moves one value in some thousands to the other fp16 neighbour, and through it one 8-bit code in 10^5; the fp64 one gives the
 // definition's bits; the vector units are idle beside it all the same (27.6 million instructions of 16384 wavefronts in 70 us).
-// Bound: memory.  Two prompts of 8192 and 4096 tokens, 32 + 2 x 8 heads of 128 dimensions, into int8: 324 MB in 70 us, 4.6 TB/s (a copy
+// Bound: memory.  Two prompts of 8192 and 6144 tokens, 32 + 2 x 8 heads of 128 dimensions, into int8: 324 MB in 70 us, 4.6 TB/s (a copy
 // reaches 4.8).  With few tokens the launch: one token 3.6 us on the GPU, so its heads are spread over more workgroups.
 struct AppendArgs {
     const uint16_t *qkv;
