@@ -334,6 +334,22 @@ def test_long_cache():
         c.check()
 
 
+# one part; parts joined by the last workgroup (a few values, many values of many row blocks); by the join kernel, with two and with all of
+# a workgroup's threads to a row; as many parts as there may be, joined either way; with forms of the score
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("nq,nkv,d,L,T,window", [(4, 2, 128, 380, 4, 0), (4, 2, 128, 381, 4, 0), (8, 2, 128, 900, 1, 0), (32, 32, 128, 1100, 16, 0),
+                                                 (16, 2, 128, 600, 16, 0), (8, 1, 64, 2500, 9, 0), (1, 1, 64, 70000, 1, 0), (8, 1, 64, 66000, 4, 0),
+                                                 (8, 2, 64, 3000, 2, 2900), (8, 2, 64, 3000, 20, 1300)], ids=str)
+def test_every_way_to_divide(fmt, nq, nkv, d, L, T, window):
+    _say(fmt, nq, nkv, d, "L", L, "T", T, "window", window)
+    c = Case(fmt, nq, nkv, d, [L], T, window=window, seed=41)
+    c.poison_rest()
+    first = c.check()
+    c.call()                                                        # (the counters of the row blocks are as they were)
+    torch.cuda.synchronize()
+    assert np.array_equal(first, c.out.cpu().numpy())
+
+
 def test_one_handle_for_calls_of_different_sizes():
     big = Case("f16", 8, 2, 64, [700, 100], 40, seed=20)
     small = Case("f16", 8, 2, 64, [30, 9], 2, seed=21, max_tokens=40, extra=big.rows - 32)
