@@ -316,6 +316,11 @@ struct Part {
         const int first = lo / STEP, steps = (sq.end + STEP - 1) / STEP - first, per = (steps + a.splits - 1) / a.splits;
         begin = first + at.split * per, end = min(first + steps, begin + per);
     }
+    // Step i of the part, or the last one if there is none.  With forms from the last key to the first: under a bias that falls with the
+    // distance the last keys have the largest scores, and references then move once and not in every step (one token over 2048 fp16 rows, one part
+    // 35 -> 23 us).  Without forms from the first to the last: the step with the masks, which wait for LDS, does not come first (7 % over 256 rows).
+    __device__ __forceinline__ bool has(int i) const { return i < end - begin; }
+    __device__ __forceinline__ int at(int i) const { return FORMS ? max(end - 1 - i, begin) : min(begin + i, end - 1); }
 };
 
 // Queries of a row as B operands (dims(ks): first dimension of this lane's eight in contraction step ks) and what else a row has.
@@ -543,8 +548,8 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     auto load_scale = [&](int step) {
         if constexpr (SCALED) scale = scale_src[min(step * kStep + (lane & 31), sq.end - 1)];
     };
-    int step = part.begin + wv;
-    if (step < part.end) {
+    int step = part.at(wv);
+    if (part.has(wv)) {
         load_scale(step);
         keys.load(kr, koff + (uint32_t)step * (kStep * ROW));
         vals.load(vr, voff + (uint32_t)step * (kStep * ROW));
@@ -553,10 +558,10 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
         fill<FORMS, NT>(a, sq, first_row, live, look_up);
         lds_barrier();
     }
-    for (; step < part.end; step += NW) {
+    for (int i = wv; part.has(i); i += NW) {
         const int j0 = step * kStep;
         const bool masked = j0 + kStep > sq.len || j0 < part.all_from;      // (the same for the whole wavefront)
-        const int next = min(step + NW, part.end - 1);
+        const int next = part.at(i + NW);
         if constexpr (SCALED) {
             const float x = lane < 32 ? scale * to_score : at_least_small(scale);
             scales[wv][lane >> 5][lane & 31] = x;
@@ -600,6 +605,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
                 for (int r = 0; r < NR; ++r) sum[r].acc[2 * pair + j] = mfma16(v[j], w[r], sum[r].acc[2 * pair + j]);
         }
         vals.load(vr, voff + (uint32_t)next * (kStep * ROW));
+        step = next;
     }
 
     // ---- the wavefronts' results joined, 16 rows at a time
@@ -756,8 +762,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         if (SCALED && wv < 2) scale = scale_src[min(step * kBlockStep + lane, sq.end - 1)];
     };
     auto masked_step = [&](int step) { return (step + 1) * kBlockStep > sq.len || step * kBlockStep < part.all_from; };
-    auto write = [&](int step) {
-        const int buf = (step - part.begin) & 1;
+    auto write = [&](int i) {
+        const int buf = i & 1, step = part.at(i);
         const bool look = FMT != CF_CACHE_INT8 && masked_step(step);
         uint32_t odd = 0;
         auto put = [&](char *rows, int row_bytes, u32x4 raw, int piece, bool check) {
@@ -785,20 +791,20 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     };
     if (tid < 2) lds.unfit[tid] = 0;
     if (part.begin < part.end) {
-        request(part.begin);
+        request(part.at(0));
         if (part.end * kBlockStep > sq.len) fill<FORMS, T>(a, sq, first_row, live, look_up);
         lds_barrier();
-        write(part.begin);
-        request(min(part.begin + 1, part.end - 1));
+        write(0);
+        request(part.at(1));
     }
-    for (int step = part.begin; step < part.end; ++step) {
+    for (int i = 0; part.has(i); ++i) {
         lds_barrier();                                              // this step is written, and the other buffer has been read
-        if (step + 1 < part.end) {
-            write(step + 1);
-            request(min(step + 2, part.end - 1));
+        if (part.has(i + 1)) {
+            write(i + 1);
+            request(part.at(i + 2));
         }
         if (my_rows >= live) continue;                              // a wavefront without rows only stages
-        const int buf = (step - part.begin) & 1, j0 = step * kBlockStep;
+        const int buf = i & 1, step = part.at(i), j0 = step * kBlockStep;
         const char *kb = lds.k[buf], *vb = lds.v[buf];
         const bool masked = masked_step(step);
 #pragma unroll
@@ -971,10 +977,11 @@ constexpr int kJoinedInPlace = 10240, kManyInPlace = 16384, kManyBlocks = 32;
 // so that the best number of parts grows with the root of the keys: sqrt(keys / 24) for plain scores.  (One token, 8 KV heads, int8, 8 / 16 / 32
 // parts: 2048 rows 8.7 / 8.9 / 9.7 us, 8192 rows 13.1 / 11.3 / 12.3.)  The join kernel costs about the same for any number: three times as
 // many keys under the root.  (One token, 64 heads, fp16, 4096 rows: 12 / 16 / 24 / 32 parts 11.7 / 11.5 / 10.6 / 10.5.)  Scores with forms take
-// twice the time per key.  No more than give every compute unit a workgroup, or, where parts then still have 1024 keys, the eight
-// wavefronts that it holds (32 tokens over 8192 int8 rows, batch 4, 2 / 4 parts 37.6 / 32.5 us; 64 tokens over 4096 e4m3 rows, 32 heads, 4 / 8
-// parts 17.7 / 20.6).  Never fewer than 128 keys, and one part up to 384 keys where a workgroup has at most 64 rows: nothing to join
-// saves 0.7 to 1.7 us.  Parts are whole multiples of 128 keys, so that all wavefronts have as many steps.
+// twice the time per key.  No more parts than leave every workgroup a compute unit (280 workgroups on 256 units 16.0 us, 252 13.7: 16 tokens over
+// 4096 rows with forms, 14 / 7 heads, batch 2), or, where parts then still have 1024 keys, than fill the eight wavefronts that a unit
+// holds (32 tokens over 8192 int8 rows, batch 4, 2 / 4 parts 37.6 / 32.5 us; 64 tokens over 4096 e4m3 rows, 32 heads, 4 / 8 parts
+// 17.7 / 20.6).  Never fewer than 128 keys, and one part up to 384 keys (192 with forms) where a workgroup has at most 64 rows: nothing to
+// join saves 0.7 to 1.7 us.  Parts are whole multiples of 128 keys, so that all wavefronts have as many steps.
 Plan plan_of(const cf_cache_config &c, bool forms, int batch, int tokens, int keys, int cus, int limit)
 {
     const auto &shapes = shapes_of(c, forms);
@@ -984,7 +991,7 @@ Plan plan_of(const cf_cache_config &c, bool forms, int batch, int tokens, int ke
     const Shape &shape = shapes[p.shape];
     p.blocks = (live + shape.rows - 1) / shape.rows;
     const long long items = (long long)batch * c.n_kv_heads * p.blocks;
-    const auto fill = [&](long long places) { return (int)((places + items - 1) / items); };
+    const auto fill = [&](long long places) { return (int)std::max(places / items, 1ll); };
     const auto in_place = [&](int parts) {
         const long long values = (long long)parts * (live < shape.rows ? live : shape.rows) * c.head_dim;
         return values <= kJoinedInPlace || (values <= kManyInPlace && items >= kManyBlocks);
@@ -996,7 +1003,7 @@ Plan plan_of(const cf_cache_config &c, bool forms, int batch, int tokens, int ke
     int few = in_rounds(most / std::sqrt(work / 24) + 0.5);
     if (!in_place(few)) few = in_rounds(most / std::sqrt(work / 8));
     const int wanted = keys / 1024 < few ? few : keys / 1024 < full ? keys / 1024 : full;
-    p.splits = keys <= 384 && shape.rows <= 64 ? 1 : std::min(wanted, most);
+    p.splits = work <= 384 && shape.rows <= 64 ? 1 : std::min(wanted, most);
     if (p.splits > kMaxSplits) p.splits = kMaxSplits;
     if (limit > 0) p.splits = p.splits > limit ? limit : p.splits;
     if (p.splits < 1) p.splits = 1;
@@ -1029,8 +1036,8 @@ int cf_tree_create(const cf_tree_config *cfg, cf_tree *out)
     if (hipGetDevice(&dev) != hipSuccess ||
         hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
         return CF_EHIP;
-    // Rows of partial results: a call with more than one part has fewer than twice as many workgroups as there are places for them, two
-    // to a compute unit up to 128 rows a workgroup, one with 256.
+    // Rows of partial results: a call with more than one part has no more workgroups than there are places for them, two to a compute
+    // unit up to 128 rows a workgroup, one with 256, and set_splits only takes some away.  Twice that.
     const size_t rows = 4 * (size_t)cus * 128;
     const uint32_t counters = 4 * (uint32_t)cus;                    // row blocks of a call with more than one part: fewer than workgroups
     cf_tree t = new (std::nothrow) cf_tree_s();
