@@ -37,7 +37,7 @@ constexpr int kStep = 32;                  // keys of a step
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -1e30f;            // mm of a row that has seen nothing
 constexpr float kSmallScale = 0x1p-60f;    // stands for smaller scales: no fp16 result shows values of 448 times that
-constexpr float kMostWeight = 32768.f, kMoveFrom = 14.5f, kTopExponent = 7.f;
+constexpr float kMostWeight = 32768.f, kTopExponent = 7.f;
 
 struct TreeArgs {
     const uint16_t *q;
@@ -195,8 +195,10 @@ struct Sums {
 };
 
 // The weights of NR rows for two tiles of 16 keys from j0 on, as B operands of the second product.  masked: some row of the workgroup does
-// not see all of these keys.  careful: some reference is so large that x_j - mm has to be the difference of rounded numbers (the fused
-// multiply-add keeps bits of x_j that mm, which was taken from a rounded one, lacks: above 2^24 that is whole powers of two).
+// not see all of these keys.  Where a row's reference is large, x_j - mm has to be the difference of rounded numbers (the fused multiply-add
+// keeps bits of x_j that mm, which was taken from a rounded one, lacks: above 2^24 that is whole powers of two); careful: some row of the
+// wavefront has such a reference, and each row looks at its own.  Whether a row moves its reference, and to where, is its own matter as well:
+// the other rows of the wavefront go through the second pass with the weights that they had.
 constexpr float kCareful = 0x1p20f;
 template <int HD, int FMT, bool FORMS, int NR>
 __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row (&row)[NR], int g, int j0, bool masked, bool &careful,
@@ -204,18 +206,25 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
                                       h8 (&w)[NR])
 {
     constexpr bool SCALED = FMT != CF_CACHE_F16;
-    float add[NR];
+    float add[NR], most[NR];
     for (int pass = 0;; ++pass) {
-        float most = 0.f;
+        float highest = 0.f;
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             float p[8], wt[8];
             if (FORMS || masked || careful) {
+                const bool large = fabsf(sum[r].mm) > kCareful;
                 arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], kscale, p);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const bool none = p[e] == -INFINITY;
-                    p[e] = exp2_(p[e] - sum[r].mm);
+                    const bool none = (FORMS || masked) && p[e] == -INFINITY;
+                    const float rounded = p[e] - sum[r].mm;
+                    float y = rounded;
+                    if (!FORMS && !masked) {
+                        const float fused = fmaf(s[r][e >> 2][e & 3], SCALED ? kscale[e >> 2][e & 3] : to_score, -sum[r].mm);
+                        y = large ? rounded : fused;
+                    }
+                    p[e] = exp2_(y);
                     wt[e] = SCALED ? (none ? 0.f : p[e] * vscale[e >> 2][e & 3]) : p[e];       // (the scale of an unseen row may be anything)
                 }
             } else {
@@ -226,17 +235,18 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
                 }
             }
             add[r] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-            most = fmaxf(fmaxf(most, wt[0]), wt[1]);
+            most[r] = fmaxf(wt[0], wt[1]);
 #pragma unroll
-            for (int e = 2; e < 8; e += 2) most = fmaxf(fmaxf(most, wt[e]), wt[e + 1]);
+            for (int e = 2; e < 8; e += 2) most[r] = fmaxf(fmaxf(most[r], wt[e]), wt[e + 1]);
+            highest = fmaxf(highest, most[r]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[r][e] = (_Float16)wt[e];
         }
-        if (pass || !__any(most > kMostWeight)) break;
+        if (pass || !__any(highest > kMostWeight)) break;
         // some weight is too large: rows with such a one get a new reference, and all weights are taken again
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            float x[8], top = kNone, over = 0.f;
+            float x[8], top = kNone;
             arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], kscale, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -244,13 +254,13 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
                 top = fmaxf(top, y);
             }
             top = cf::lanes::max_groups<16>(top);
-            over = top - sum[r].mm;
-            const float to = over > kMoveFrom ? top - kTopExponent : sum[r].mm, by = exp2_(sum[r].mm - to);
+            const bool moves = cf::lanes::max_groups<16>(most[r]) > kMostWeight;
+            const float to = moves ? top - kTopExponent : sum[r].mm, by = moves ? exp2_(sum[r].mm - to) : 1.f;
             sum[r].mm = to;
             sum[r].l *= by;
 #pragma unroll
             for (int j = 0; j < HD / 16; ++j) sum[r].acc[j] *= by;
-            careful = careful || __any(to > kCareful || (to < -kCareful && to != kNone));
+            careful = careful || __any(moves && fabsf(to) > kCareful);
         }
     }
 #pragma unroll
