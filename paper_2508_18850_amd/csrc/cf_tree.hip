@@ -85,6 +85,9 @@ __device__ __forceinline__ uint32_t seen_bits(bool tree, int words, const uint64
 __device__ __forceinline__ float at_least_small(float x) { return x != x ? x : fmaxf(x, kSmallScale); }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+// A factor of sums of weighted values that an infinity among them outlives.  (The sums are below 2^55, and 2^-126 of one is below 2^-70: no result
+// shows it, with scales of values that fp16 holds.)
+__device__ __forceinline__ float for_sums(float f) { return fmaxf(f, 0x1p-126f); }
 
 __device__ __forceinline__ void wave_sync()
 {
@@ -158,7 +161,7 @@ __device__ __forceinline__ float tanh_(float x)
 // Arguments x_j of a row for two tiles of 16 keys from j0 on; minus infinity for a key that it does not see.
 template <int FMT, bool FORMS>
 __device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row &row, int g, int j0, bool masked, float to_score,
-                                          const f32x4 (&s)[2], const f32x4 (&kscale)[2], float (&x)[8])
+                                          const f32x4 (&s)[2], const f32x4 (&kscale)[2], float (&x)[8], bool (&sees)[8])
 {
     const uint32_t bits = masked ? seen_bits(sq.tree != nullptr, a.words, row.mask, row.tok, j0, sq.len, sq.n) : ~0u;
 #pragma unroll
@@ -179,6 +182,7 @@ __device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq,
             if (masked && a.window > 0) seen = seen && distance < a.window;
         }
         x[e] = seen ? x[e] : -INFINITY;
+        sees[e] = seen;
     }
 }
 
@@ -212,12 +216,12 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             float p[8], wt[8];
+            bool sees[8];
             if (FORMS || masked || careful) {
                 const bool large = fabsf(sum[r].mm) > kCareful;
-                arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], kscale, p);
+                arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], kscale, p, sees);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const bool none = (FORMS || masked) && p[e] == -INFINITY;
                     const float rounded = p[e] - sum[r].mm;
                     float y = rounded;
                     if (!FORMS && !masked) {
@@ -225,7 +229,7 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
                         y = large ? rounded : fused;
                     }
                     p[e] = exp2_(y);
-                    wt[e] = SCALED ? (none ? 0.f : p[e] * vscale[e >> 2][e & 3]) : p[e];       // (the scale of an unseen row may be anything)
+                    wt[e] = SCALED ? (sees[e] ? p[e] * vscale[e >> 2][e & 3] : 0.f) : p[e];       // (the scale of an unseen row may be anything)
                 }
             } else {
 #pragma unroll
@@ -247,7 +251,8 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             float x[8], top = kNone;
-            arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], kscale, x);
+            bool sees[8];
+            arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], kscale, x, sees);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float y = x[e] == -INFINITY ? kNone : SCALED ? x[e] + __builtin_amdgcn_logf(vscale[e >> 2][e & 3]) : x[e];
@@ -259,7 +264,7 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
             sum[r].mm = to;
             sum[r].l *= by;
 #pragma unroll
-            for (int j = 0; j < HD / 16; ++j) sum[r].acc[j] *= by;
+            for (int j = 0; j < HD / 16; ++j) sum[r].acc[j] *= for_sums(by);
             careful = careful || __any(moves && fabsf(to) > kCareful);
         }
     }
@@ -267,19 +272,38 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
     for (int r = 0; r < NR; ++r) sum[r].l += add[r];
 }
 
-// Value rows with infinities or NaN that some row does not see would enter its product as 0 times that.  Where a step holds one, such
-// values are left out of the product, and this adds them, key by key, to the rows that see them.  dim(j, rr): dimension of acc[j][rr].
-template <int HD, int FMT, typename Dim>
-__device__ __forceinline__ void add_unfit(__amdgpu_buffer_rsrc_t vr, int j0, int c, const h8 &w, f32x4 (&acc)[HD / 16], Dim dim)
+// A value that is infinite or NaN, and that a row sees, makes that dimension of its result infinite or NaN, however small the weight: the
+// weight of a key that a row sees is more than 0, though fp16 and fp32 may not hold it.  Products would give 0 times infinity there, and also
+// to the rows that do not see the key.  So steps in which some row does not see all keys leave such values out of the product (unfit: there
+// was one), and a wavefront that left some out, or has sums that are not finite, looks over its steps once more at the end and puts
+// into the sums of each row the infinities and NaN that it sees.  From there on no factor of a sum is 0 (for_sums).
+template <int HD, int NR>
+__device__ __forceinline__ bool not_finite(const Sums<HD> (&sum)[NR])
+{
+    f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j) z += sum[r].acc[j] * 0.f;
+    return __any((z[0] + z[1]) + (z[2] + z[3]) != 0.f);
+}
+// The 32 keys from j0 on, for one row.  dim(j, rr): dimension of acc[j][rr].
+template <int HD, int FMT, bool FORMS, typename Dim>
+__device__ __forceinline__ void put_unfit(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row &row, __amdgpu_buffer_rsrc_t vr, int j0, int c, int g,
+                                          f32x4 (&special)[HD / 16], Dim dim)
 {
     constexpr int ROW = HD * kValueBytes<FMT>;
+    Values<HD, FMT> vals;
+    vals.load(vr, Values<HD, FMT>::offset(c, g) + (uint32_t)j0 * ROW);
+    if (!__any(vals.take_out_unfit())) return;
+    const uint32_t bits = seen_bits(sq.tree != nullptr, a.words, row.mask, row.tok, j0, sq.len, sq.n);
 #pragma unroll 1
     for (int i = 0; i < 32; ++i) {
-        const int element = 4 * (i >> 4) + (i & 3);                 // key i is this element of lane group (i / 4) % 4
-        float wt = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) wt = e == element ? (float)w[e] : wt;
-        wt = __shfl(wt, 16 * ((i >> 2) & 3) + c);
+        bool seen = bits >> i & 1;
+        if (FORMS && a.window > 0) {
+            const int key_at = j0 + i < sq.len ? j0 + i : new_at[min(j0 + i - sq.len, sq.n - 1)];
+            seen = seen && row.at - key_at < a.window;
+        }
 #pragma unroll
         for (int j = 0; j < HD / 16; ++j)
 #pragma unroll
@@ -293,9 +317,18 @@ __device__ __forceinline__ void add_unfit(__amdgpu_buffer_rsrc_t vr, int j0, int
                     decode4<FMT>((uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(vr, at, 0, 0), f);
                     x = f[0];
                 }
-                acc[j][rr] += (!(fabsf(x) <= 65504.f) && wt != 0.f) ? wt * x : 0.f;
+                special[j][rr] += seen && !(fabsf(x) <= 65504.f) ? x : 0.f;
             }
     }
+}
+// Sums of a row with what put_unfit found.
+template <int HD>
+__device__ __forceinline__ void take_over(const f32x4 (&special)[HD / 16], f32x4 (&acc)[HD / 16])
+{
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) acc[j][rr] = special[j][rr] == 0.f ? acc[j][rr] : special[j][rr];
 }
 // Where a workgroup works: workgroup i runs on die i mod 8, and the row blocks of a unit (a sequence's head and part), which read the same
 // keys and values, follow each other on one die.
@@ -445,7 +478,7 @@ __device__ __forceinline__ void join_rows(const TreeArgs &a, const Place &at, in
                     m = to;
                     total = total * old + (there ? f * x[i].y : 0.f);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) o[h] = o[h] * old + (there ? u[i][h] * f : f32x4{0.f, 0.f, 0.f, 0.f});
+                    for (int h = 0; h < 2; ++h) o[h] = o[h] * for_sums(old) + (there ? u[i][h] * for_sums(f) : f32x4{0.f, 0.f, 0.f, 0.f});
                 }
             }
         };
@@ -480,7 +513,7 @@ __device__ __forceinline__ void join_rows(const TreeArgs &a, const Place &at, in
                 const float2 y = space.ml[mine * lanes + s];
                 const float f = exp2_(y.x - top);
                 sum += f * y.y;
-                x += *reinterpret_cast<const f32x4 *>(&space.sums[mine * lanes + s][d]) * f;
+                x += *reinterpret_cast<const f32x4 *>(&space.sums[mine * lanes + s][d]) * for_sums(f);
             }
             const float inv = sum == 0.f ? 0.f : unit_v / sum;
             typedef _Float16 h4 __attribute__((ext_vector_type(4)));
@@ -553,7 +586,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     Values<HD, FMT> vals;
     float scale = 0.f;
     Sums<HD> sum[NR];
-    bool careful = false;
+    bool careful = false, unfit = false;
     const uint32_t koff = Keys<HD, FMT>::offset(c, g), voff = Values<HD, FMT>::offset(c, g);
     auto load_scale = [&](int step) {
         if constexpr (SCALED) scale = scale_src[min(step * kStep + (lane & 31), sq.end - 1)];
@@ -601,9 +634,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
         h8 w[NR];
         weigh<HD, FMT, FORMS, NR>(a, sq, look_up.at, row, g, j0, masked, careful, to_score, s, kscale, vscale, sum, w);
         // ---- values
-        if (FMT != CF_CACHE_INT8 && masked && __any(vals.take_out_unfit()))
-#pragma unroll
-            for (int r = 0; r < NR; ++r) add_unfit<HD, FMT>(vr, j0, c, w[r], sum[r].acc, [&](int j, int rr) { return NJ * (4 * g + rr) + j; });
+        if (FMT != CF_CACHE_INT8 && masked) unfit = __any(vals.take_out_unfit()) || unfit;
         vals.flip();
 #pragma unroll
         for (int pair = 0; pair < NJ / 2; ++pair) {
@@ -617,6 +648,15 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
         vals.load(vr, voff + (uint32_t)next * (kStep * ROW));
         step = next;
     }
+
+    if (FMT != CF_CACHE_INT8 && (unfit || not_finite(sum)))
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            f32x4 special[NJ] = {};
+            for (int i = wv; part.has(i); i += NW)
+                put_unfit<HD, FMT, FORMS>(a, sq, look_up.at, row[r], vr, part.at(i) * kStep, c, g, special, [&](int j, int rr) { return NJ * (4 * g + rr) + j; });
+            take_over<HD>(special, sum[r].acc);
+        }
 
     // ---- the wavefronts' results joined, 16 rows at a time
 #pragma unroll
@@ -647,7 +687,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
                 const float *src = smem + (k * 16 + row16) * (HD + 4) + d0;
                 total += f * ml[k][i].y;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] += f * src[e];
+                for (int e = 0; e < 8; ++e) o[e] += for_sums(f) * src[e];
             }
             if (a.splits > 1) {
                 const Partials to(a, HD);
@@ -756,7 +796,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
 
     Sums<HD> sum[NR];
-    bool careful = false;
+    bool careful = false, unfit = false;
 
     // ---- staging: requested a step ahead of the one that is written, which is a step ahead of the one that is used
     u32x4 kraw[PIECES], vraw[PIECES];
@@ -817,6 +857,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         const int buf = i & 1, step = part.at(i), j0 = step * kBlockStep;
         const char *kb = lds.k[buf], *vb = lds.v[buf];
         const bool masked = masked_step(step);
+        if (FMT != CF_CACHE_INT8 && masked) unfit = __builtin_amdgcn_readfirstlane(lds.unfit[buf]) == 1 + step || unfit;
 #pragma unroll
         for (int h = 0; h < 2 / KG; ++h) {
             const int half = KG == 2 ? my_half : h;
@@ -839,9 +880,6 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
             }
             h8 w[NR];
             weigh<HD, FMT, FORMS, NR>(a, sq, look_up.at, row, g, j0 + 32 * half, masked, careful, to_score, s, kscale, vscale, sum, w);
-            if (FMT != CF_CACHE_INT8 && masked && __builtin_amdgcn_readfirstlane(lds.unfit[buf]) == 1 + step)
-#pragma unroll
-                for (int r = 0; r < NR; ++r) add_unfit<HD, FMT>(vr, j0 + 32 * half, c, w[r], sum[r].acc, [&](int j, int rr) { return 16 * j + 4 * g + rr; });
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 const h8 v = transposed<S::VROW>(vb, 32 * half, 16 * j, c, g);
@@ -850,6 +888,18 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
             }
         }
     }
+
+    if (FMT != CF_CACHE_INT8 && (unfit || not_finite(sum)))
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            f32x4 special[NJ] = {};
+            for (int i = 0; part.has(i); ++i)
+#pragma unroll 1
+                for (int h = 0; h < 2 / KG; ++h)
+                    put_unfit<HD, FMT, FORMS>(a, sq, look_up.at, row[r], vr, part.at(i) * kBlockStep + 32 * (KG == 2 ? my_half : h), c, g, special,
+                                              [&](int j, int rr) { return 16 * j + 4 * g + rr; });
+            take_over<HD>(special, sum[r].acc);
+        }
 
 #pragma unroll
     for (int r = 0; r < NR; ++r) sum[r].l = cf::lanes::sum_groups<16>(sum[r].l);
@@ -877,7 +927,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
                 sum[r].mm = to;
                 sum[r].l = sum[r].l * mine + x.y * theirs;
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) sum[r].acc[j] = sum[r].acc[j] * mine + *reinterpret_cast<const f32x4 *>(other + i * STRIDE + 16 * j + 4 * g) * theirs;
+                for (int j = 0; j < NJ; ++j) sum[r].acc[j] = sum[r].acc[j] * for_sums(mine) + *reinterpret_cast<const f32x4 *>(other + i * STRIDE + 16 * j + 4 * g) * for_sums(theirs);
             }
     }
 #pragma unroll

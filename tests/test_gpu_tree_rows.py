@@ -102,3 +102,94 @@ def test_another_tokens_large_scores(fmt, T):
     assert np.abs(np.einsum("bthd,bhjd->bthj", c.q[:, 1::2].astype(np.float64), c.kv[:, :, :L])).max(-1).min() / 8 > 2 ** 20
     loud = c.run()
     assert np.array_equal(quiet[:, 0::2], loud[:, 0::2])
+
+
+# ---- infinities and NaN among the values ---------------------------------------------------------------------------------
+
+def _unfit(fmt):
+    """What to put among the values: (as stored, as seen in the result)."""
+    if fmt == "f16":
+        return [(np.float16(x), x) for x in (np.inf, -np.inf, np.nan)]
+    return [(0x7f, np.nan), (0xff, np.nan)]
+
+
+@pytest.mark.parametrize("fmt", ["f16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", SIZES)
+@pytest.mark.parametrize("window", [0, 10000])
+def test_infinite_values_with_small_weights(fmt, d, T, window):
+    """A seen value that is infinite or NaN shows in the result, whatever its weight: e^-21 and e^-250 of the largest (less than fp16 and
+    less than fp32 hold), before and behind the key that has the largest, in steps that all tokens see and in steps that they do not,
+    in a part with the largest and in another one.  The other dimensions, and the tokens that do not see it, keep their bits."""
+    mask = np.zeros((T, T), bool)
+    mask[::2, 2] = True
+    c = _shaped(fmt, T, mask=mask, window=window, d=d)
+    for gap in (21.0, 250.0):
+        c.first = np.random.default_rng(9).uniform(-0.25, 0.25, c.rows)
+        c.first[200] = gap
+        _put(c)
+        for splits in (1, 3):
+            c.tree.set_splits(splits)
+            clean = c.run()
+            for at, sees in ((10, slice(None)), (250, slice(None)), (L - 1, slice(None)), (L + 2, slice(0, None, 2))):
+                for stored, seen in _unfit(fmt):
+                    before = c.v[0, :, at, 5].copy()
+                    c.v[0, :, at, 5] = stored
+                    want = clean.copy()
+                    want[:, sees, :, 5] = seen
+                    got = c.run()
+                    assert np.array_equal(got, want, equal_nan=True), (gap, splits, at, seen)
+                    c.v[0, :, at, 5] = before
+
+
+@pytest.mark.parametrize("T", SIZES)
+def test_infinities_of_both_signs(T):
+    """Seen together they are NaN; the token that sees one of them gets that one."""
+    mask = np.zeros((T, T), bool)
+    mask[::2, 2] = True
+    c = _shaped("f16", T, mask=mask)
+    c.first[200] = 250.0
+    _put(c)
+    c.v[0, :, 10, 5], c.v[0, :, L + 2, 5] = np.inf, -np.inf
+    got = c.run()
+    assert np.isnan(got[:, ::2, :, 5]).all() and (got[:, 1::2, :, 5] == np.inf).all()
+    keep = [i for i in range(64) if i != 5]
+    assert np.isfinite(got[..., keep]).all()
+
+
+@pytest.mark.parametrize("T", SIZES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_unseen_rows_may_hold_nan_codes(T, d):
+    """e4m3 codes that are NaN, in keys and values of a drafted token, and in cached rows outside a window."""
+    mask = np.zeros((T, T), bool)
+    mask[:, 4] = mask[1::2, 5] = True
+    c = _shaped("e4m3", T, mask=mask, d=d)
+    _put(c)
+    clean = c.check()
+    c.k[0, :, L + 5], c.v[0, :, L + 5] = 0x7f, 0xff
+    got = c.run()
+    assert np.array_equal(got[:, 0::2], clean[:, 0::2]) and np.isnan(got[:, 1::2]).all()
+    depth = np.full(T, 10, np.int32)
+    depth[1::2] = 2
+    c = _shaped("e4m3", T, window=L + 10 - 140, depth=depth, d=d)
+    _put(c)
+    clean = c.check()
+    c.k[0, :, 140], c.v[0, :, 140] = 0xff, 0x7f
+    got = c.run()
+    assert np.array_equal(got[:, 0::2], clean[:, 0::2]) and np.isnan(got[:, 1::2]).all()
+    c.k[0, :, :140], c.v[0, :, :140] = 0x7f, 0x7f                   # what no token sees
+    assert np.array_equal(c.run()[:, 0::2], clean[:, 0::2])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("T", SIZES)
+def test_a_nan_scale_with_a_small_weight(fmt, T):
+    """A seen row of values with scale NaN is NaN in every dimension, however small its weight."""
+    c = _shaped(fmt, T)
+    c.first[200] = 250.0
+    _put(c)
+    for at in (10, 250, L - 1):
+        before = c.vs[0, :, at].copy()
+        c.vs[0, :, at] = np.nan
+        assert np.isnan(c.run()).all(), at
+        c.vs[0, :, at] = before
