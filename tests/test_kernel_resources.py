@@ -84,3 +84,11 @@ def test_counters_are_not_read_as_constants(tmp_path):
     text = ir.read_text()
     assert "fused_ffn_tiles" in text
     assert not re.findall(r"(?:inttoptr|addrspacecast) .* to ptr addrspace\(4\)", text)
+
+
+def test_tree_attention_has_no_scratch():
+    """Its wavefronts keep queries, sums and the next step's keys and values in registers; copies to memory would wait for each other there."""
+    mine = {k: v for k, v in kernels().items() if "tree_tiles" in k or "tree_blocks" in k or "tree_join" in k}
+    assert len([k for k in mine if "tree_tiles" in k]) == 18 and len([k for k in mine if "tree_join" in k]) == 2
+    for name, kernel in mine.items():
+        assert kernel[".private_segment_fixed_size"] == 0 and kernel[".vgpr_spill_count"] == 0, name
