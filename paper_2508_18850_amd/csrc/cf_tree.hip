@@ -20,6 +20,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <type_traits>
 
@@ -1027,6 +1028,19 @@ KernelFn pick(int hd, int fmt, int shape, bool forms)
     return forms ? pick_format<128, true>(fmt, shape) : pick_format<128, false>(fmt, shape);
 }
 
+// shape for `live` rows of a KV head, and the rows of its row blocks
+int shape_of(int live)
+{
+    int i = 0;
+    while (i < kShapes - 1 && live > 16 << i) ++i;
+    return i;
+}
+int block_rows(const Shape (&shapes)[kShapes], int live)
+{
+    const int rows = shapes[shape_of(live)].rows;
+    return (live + rows - 1) / rows * rows;
+}
+
 constexpr int kMaxSplits = 64;
 // Parts that the last workgroup of a row block joins by itself have at most this many values (fp32) together, where there are many row
 // blocks, whose join kernel would read as much again, the second number.  (Against the join kernel: up to 4096 values -0.7 us, 8192 to 10240
@@ -1047,9 +1061,9 @@ Plan plan_of(const cf_cache_config &c, bool forms, int batch, int tokens, int ke
     const auto &shapes = shapes_of(c, forms);
     const int live = tokens * (c.n_q_heads / c.n_kv_heads);
     Plan p;
-    for (p.shape = 0; p.shape < kShapes - 1 && live > 16 << p.shape;) ++p.shape;
+    p.shape = shape_of(live);
     const Shape &shape = shapes[p.shape];
-    p.blocks = (live + shape.rows - 1) / shape.rows;
+    p.blocks = block_rows(shapes, live) / shape.rows;
     const long long items = (long long)batch * c.n_kv_heads * p.blocks;
     const auto fill = [&](long long places) { return (int)std::max(places / items, 1ll); };
     const auto in_place = [&](int parts) {
@@ -1069,6 +1083,20 @@ Plan plan_of(const cf_cache_config &c, bool forms, int batch, int tokens, int ke
     if (p.splits < 1) p.splits = 1;
     p.in_place = in_place(p.splits);
     return p;
+}
+
+// Rows of partial results that no call of this configuration exceeds.  A call with more than one part has no more workgroups than there are
+// places for them (plan_of), two to a compute unit up to 128 rows a workgroup, one with 256, and set_splits only takes some away.  And none
+// has more rows than the largest batch with the most tokens (the rows of all row blocks grow with the tokens), nor more parts than 128 keys
+// each leave.
+size_t partial_rows(const cf_tree_config &t, int cus)
+{
+    const cf_cache_config &c = t.cache;
+    const int live = t.max_tokens * (c.n_q_heads / c.n_kv_heads);
+    size_t padded = 0;
+    for (const bool forms : {false, true}) padded = std::max(padded, (size_t)block_rows(shapes_of(c, forms), live));
+    const size_t parts = std::min((c.max_seq + 4 * kStep - 1) / (4 * kStep), kMaxSplits);
+    return std::min(2 * (size_t)cus * 128, (size_t)c.max_batch * c.n_kv_heads * padded * parts);
 }
 
 }  // namespace
@@ -1096,10 +1124,8 @@ int cf_tree_create(const cf_tree_config *cfg, cf_tree *out)
     if (hipGetDevice(&dev) != hipSuccess ||
         hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
         return CF_EHIP;
-    // Rows of partial results: a call with more than one part has no more workgroups than there are places for them, two to a compute
-    // unit up to 128 rows a workgroup, one with 256, and set_splits only takes some away.  Twice that.
-    const size_t rows = 4 * (size_t)cus * 128;
-    const uint32_t counters = 4 * (uint32_t)cus;                    // row blocks of a call with more than one part: fewer than workgroups
+    const size_t rows = partial_rows(*cfg, cus);
+    const uint32_t counters = ((uint32_t)cus + 63) / 64 * 64;       // a call with more than one part has half as many row blocks as workgroups, at most
     cf_tree t = new (std::nothrow) cf_tree_s();
     if (!t) return CF_ENOMEM;
     t->cfg = *cfg;
