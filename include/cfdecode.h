@@ -465,8 +465,8 @@ typedef struct cf_draft {
  *
  * All calls below are asynchronous on `stream`, allocate nothing, wait for nothing and can be captured and replayed.  CF_EINVAL: a
  * null or misaligned pointer, a batch outside 1..max_batch, a cf_draft outside the limits above, a malformed cf_cache_config;
- * CF_EUNSUPPORTED: another head_dim, a head's slice of the cache of 2 GiB or more, more than 65535 heads in a call
- * (batch * n_kv_heads); CF_EHIP: the launch failed.
+ * CF_EUNSUPPORTED: another head_dim, a head's slice of the cache of 2^30 values or more (max_seq * head_dim, in every format), more than
+ * 65535 query heads, more than 65535 KV heads in a call (batch * n_kv_heads); CF_EHIP: the launch failed.
  *
  * cf_cache_append: qkv [batch, tokens, (n_q + 2 n_kv) * head_dim] fp16, columns ordered as those of W_qkv in cf_decode_block (the
  *   product of the tokens' hidden states with it); queries and keys are rotated for their positions as in cf_decode_block (angles

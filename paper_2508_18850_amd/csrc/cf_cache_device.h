@@ -45,8 +45,8 @@ inline int check_config(const cf_cache_config &c)
         !(c.rope_base <= 3.402823466e38f))
         return CF_EINVAL;
     if (c.head_dim != 64 && c.head_dim != 128) return CF_EUNSUPPORTED;
-    // 32-bit byte offsets inside a head's slice of the cache, head counts that no product of sizes overflows with
-    if (2ull * (unsigned)c.max_seq * (unsigned)c.head_dim > 0x7fffffffull || c.n_q_heads > 65535) return CF_EUNSUPPORTED;
+    // 32-bit offsets, also in bytes of fp16, inside a head's slice of the cache; head counts that no product of sizes overflows with
+    if (1ull * (unsigned)c.max_seq * (unsigned)c.head_dim >= 1ull << 30 || c.n_q_heads > 65535) return CF_EUNSUPPORTED;
     return CF_OK;
 }
 inline int check_cache(const cf_cache_config &c, const cf_cache *p, int32_t batch)
