@@ -86,9 +86,6 @@ __device__ __forceinline__ uint32_t seen_bits(bool tree, int words, const uint64
 __device__ __forceinline__ float at_least_small(float x) { return x != x ? x : fmaxf(x, kSmallScale); }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-// A factor of sums of weighted values that an infinity among them outlives.  (The sums are below 2^55, and 2^-126 of one is below 2^-70: no result
-// shows it, with scales of values that fp16 holds.)
-__device__ __forceinline__ float for_sums(float f) { return fmaxf(f, 0x1p-126f); }
 
 __device__ __forceinline__ void wave_sync()
 {
@@ -240,10 +237,10 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
                 }
             }
             add[r] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-            most[r] = fmaxf(wt[0], wt[1]);
+            most[r] = 0.f;
 #pragma unroll
-            for (int e = 2; e < 8; e += 2) most[r] = fmaxf(fmaxf(most[r], wt[e]), wt[e + 1]);
-            highest = fmaxf(highest, most[r]);
+            for (int e = 0; e < 8; e += 2) most[r] = fmaxf(fmaxf(most[r], wt[e]), wt[e + 1]);
+            highest = r ? fmaxf(highest, most[r]) : most[r];
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[r][e] = (_Float16)wt[e];
         }
@@ -265,7 +262,7 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
             sum[r].mm = to;
             sum[r].l *= by;
 #pragma unroll
-            for (int j = 0; j < HD / 16; ++j) sum[r].acc[j] *= for_sums(by);
+            for (int j = 0; j < HD / 16; ++j) sum[r].acc[j] *= by;
             careful = careful || __any(moves && fabsf(to) > kCareful);
         }
     }
@@ -275,26 +272,17 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
 
 // A value that is infinite or NaN, and that a row sees, makes that dimension of its result infinite or NaN, however small the weight: the
 // weight of a key that a row sees is more than 0, though fp16 and fp32 may not hold it.  Products would give 0 times infinity there, and also
-// to the rows that do not see the key.  So steps in which some row does not see all keys leave such values out of the product (unfit: there
-// was one), and a wavefront that left some out, or has sums that are not finite, looks over its steps once more at the end and puts
-// into the sums of each row the infinities and NaN that it sees.  From there on no factor of a sum is 0 (for_sums).
-template <int HD, int NR>
-__device__ __forceinline__ bool not_finite(const Sums<HD> (&sum)[NR])
+// to the rows that do not see the key.  So steps in which some row does not see all keys leave such values out of the product, and where some
+// were left out, or results are not finite, the threads that wrote results look over the keys once more (behind their stores, where a jump
+// across this code costs nothing) and write the infinities and NaN that their rows see.
+
+// The sums of those among P pieces of W adjacent values, from dimension d0 + 16 p on, of the 32 keys from j0 on, for one row of queries.
+template <int HD, int FMT, bool FORMS, int P, int W>
+__device__ __forceinline__ void add_unfit(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row &row, __amdgpu_buffer_rsrc_t vr, int j0, int c, int g,
+                                          int d0, float (&special)[P][W])
 {
-    f32x4 z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int r = 0; r < NR; ++r)
-#pragma unroll
-        for (int j = 0; j < HD / 16; ++j) z += sum[r].acc[j] * 0.f;
-    return __any((z[0] + z[1]) + (z[2] + z[3]) != 0.f);
-}
-// The 32 keys from j0 on, for one row.  dim(j, rr): dimension of acc[j][rr].
-template <int HD, int FMT, bool FORMS, typename Dim>
-__device__ __forceinline__ void put_unfit(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row &row, __amdgpu_buffer_rsrc_t vr, int j0, int c, int g,
-                                          f32x4 (&special)[HD / 16], Dim dim)
-{
-    constexpr int ROW = HD * kValueBytes<FMT>;
-    Values<HD, FMT> vals;
+    constexpr int VB = kValueBytes<FMT>, ROW = HD * VB, DW = W * VB / 4;
+    Values<HD, FMT> vals;                                           // is there one at all
     vals.load(vr, Values<HD, FMT>::offset(c, g) + (uint32_t)j0 * ROW);
     if (!__any(vals.take_out_unfit())) return;
     const uint32_t bits = seen_bits(sq.tree != nullptr, a.words, row.mask, row.tok, j0, sq.len, sq.n);
@@ -305,31 +293,23 @@ __device__ __forceinline__ void put_unfit(const TreeArgs &a, const Sequence &sq,
             const int key_at = j0 + i < sq.len ? j0 + i : new_at[min(j0 + i - sq.len, sq.n - 1)];
             seen = seen && row.at - key_at < a.window;
         }
+        uint32_t x[P][DW];
 #pragma unroll
-        for (int j = 0; j < HD / 16; ++j)
+        for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int rr = 0; rr < 4; ++rr) {
-                const uint32_t at = (uint32_t)(j0 + i) * ROW + dim(j, rr) * kValueBytes<FMT>;
-                float x;
-                if constexpr (FMT == CF_CACHE_F16) {
-                    x = (float)__builtin_bit_cast(_Float16, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(vr, at, 0, 0));
-                } else {
-                    float f[4];
-                    decode4<FMT>((uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(vr, at, 0, 0), f);
-                    x = f[0];
-                }
-                special[j][rr] += seen && !(fabsf(x) <= 65504.f) ? x : 0.f;
+            for (int d = 0; d < DW; ++d) x[p][d] = __builtin_amdgcn_raw_buffer_load_b32(vr, (uint32_t)(j0 + i) * ROW + (d0 + 16 * p) * VB + 4 * d, 0, 0);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                float v;
+                if constexpr (FMT == CF_CACHE_F16)
+                    v = (float)__builtin_bit_cast(_Float16, (uint16_t)(x[p][e / 2] >> 16 * (e & 1)));
+                else
+                    v = (x[p][e / 4] >> 8 * (e & 3) & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f;
+                special[p][e] += seen && !(fabsf(v) <= 65504.f) ? v : 0.f;
             }
     }
-}
-// Sums of a row with what put_unfit found.
-template <int HD>
-__device__ __forceinline__ void take_over(const f32x4 (&special)[HD / 16], f32x4 (&acc)[HD / 16])
-{
-#pragma unroll
-    for (int j = 0; j < HD / 16; ++j)
-#pragma unroll
-        for (int rr = 0; rr < 4; ++rr) acc[j][rr] = special[j][rr] == 0.f ? acc[j][rr] : special[j][rr];
 }
 // Where a workgroup works: workgroup i runs on die i mod 8, and the row blocks of a unit (a sequence's head and part), which read the same
 // keys and values, follow each other on one die.
@@ -426,6 +406,11 @@ struct Partials {
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, (row * hd + dim) * 4, 0, AUX);
     }
     template <int AUX>
+    __device__ __forceinline__ void put_one(uint32_t row, int dim, float v) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, (row * hd + dim) * 4, 0, AUX);
+    }
+    template <int AUX>
     __device__ __forceinline__ void put_ml(uint32_t row, float m, float l) const
     {
         __builtin_amdgcn_raw_buffer_store_b64(u32x2{__builtin_bit_cast(uint32_t, m), __builtin_bit_cast(uint32_t, l)}, r, ml + row * 8, 0, AUX);
@@ -441,6 +426,10 @@ struct Partials {
         return __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(r, ml + row * 8, 0, AUX));
     }
 };
+
+// A factor of a part's sums that an infinity among them outlives.  (The sums are below 2^55, and 2^-126 of one is below 2^-70: no result shows
+// it, with scales of values that fp16 holds.)
+__device__ __forceinline__ float for_sums(float f) { return fmaxf(f, 0x1p-126f); }
 
 // What T threads need to join rows.
 template <int HD, int T>
@@ -523,6 +512,31 @@ __device__ __forceinline__ void join_rows(const TreeArgs &a, const Place &at, in
         }
     }
 }
+// Over what W dimensions of row i of the workgroup's block have: the infinities and NaN that the row sees.  (A row with a NaN among its scores
+// stays NaN.)
+template <int HD, int W>
+__device__ __forceinline__ void put_special(const TreeArgs &a, const Place &at, int i, int d0, float total, const float (&special)[W])
+{
+    if (a.splits == 1) {
+        uint16_t *dst = out_row(a, at, i, HD) + d0;
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            if (special[e] != 0.f) dst[e] = __builtin_bit_cast(uint16_t, (_Float16)(special[e] + (total - total)));
+        return;
+    }
+    const Partials to(a, HD);
+    const uint32_t row = (uint32_t)at.unit * a.padded + i;
+    const auto put = [&](auto aux) {
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            if (special[e] != 0.f) to.put_one<decltype(aux)::value>(row, d0 + e, special[e]);
+    };
+    if (a.arrived)
+        put(std::integral_constant<int, kThrough>());
+    else
+        put(std::integral_constant<int, 0>());
+}
+
 // Whether this workgroup, whose partial results are on their way, is the last one of its row block; it clears the counter for the next launch.
 __device__ __forceinline__ bool last_to_arrive(const TreeArgs &a, const Place &at, int &shared)
 {
@@ -560,6 +574,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     __shared__ float2 ml[NW][16 * NR];
     __shared__ Lookup<16 * NR> look_up;
     __shared__ alignas(16) float scales[NW][2][kStep];
+    __shared__ int left_out[NW];
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
     const Place place(a);
     if (place.unit >= a.units) return;
@@ -587,7 +602,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
     Values<HD, FMT> vals;
     float scale = 0.f;
     Sums<HD> sum[NR];
-    bool careful = false, unfit = false;
+    bool careful = false, unfit = false;                            // unfit: infinities or NaN were left out of the product
     const uint32_t koff = Keys<HD, FMT>::offset(c, g), voff = Values<HD, FMT>::offset(c, g);
     auto load_scale = [&](int step) {
         if constexpr (SCALED) scale = scale_src[min(step * kStep + (lane & 31), sq.end - 1)];
@@ -650,21 +665,14 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
         step = next;
     }
 
-    if (FMT != CF_CACHE_INT8 && (unfit || not_finite(sum)))
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            f32x4 special[NJ] = {};
-            for (int i = wv; part.has(i); i += NW)
-                put_unfit<HD, FMT, FORMS>(a, sq, look_up.at, row[r], vr, part.at(i) * kStep, c, g, special, [&](int j, int rr) { return NJ * (4 * g + rr) + j; });
-            take_over<HD>(special, sum[r].acc);
-        }
-
     // ---- the wavefronts' results joined, 16 rows at a time
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         sum[r].l = cf::lanes::sum_groups<16>(sum[r].l);
         if (g == 0) ml[wv][16 * r + c] = make_float2(sum[r].mm, sum[r].l);
     }
+    if (FMT != CF_CACHE_INT8 && lane == 0) left_out[wv] = unfit;
+    float odd = 0.f;                                                // NaN where a result is not finite
     constexpr int CH = HD / 8;                                      // a thread has eight dimensions of a row
     const int row16 = tid / CH, d0 = 8 * (tid % CH);
 #pragma unroll
@@ -688,8 +696,9 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
                 const float *src = smem + (k * 16 + row16) * (HD + 4) + d0;
                 total += f * ml[k][i].y;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] += for_sums(f) * src[e];
+                for (int e = 0; e < 8; ++e) o[e] += f * src[e];
             }
+            if (FMT != CF_CACHE_INT8) odd += ((o[0] + o[1]) + (o[2] + o[3])) * 0.f + ((o[4] + o[5]) + (o[6] + o[7])) * 0.f;
             if (a.splits > 1) {
                 const Partials to(a, HD);
                 const uint32_t at = (uint32_t)place.unit * a.padded + first_row + i;
@@ -710,6 +719,23 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
             }
         }
     }
+    if constexpr (FMT != CF_CACHE_INT8) {
+        const bool all = __any(odd != 0.f);
+        if (all || __builtin_amdgcn_readfirstlane(left_out[0] | left_out[1] | left_out[2] | left_out[3])) {
+#pragma unroll 1
+            for (int r = 0; r < NR; ++r) {
+                const int i = min(16 * r + row16, live - 1);
+                const int tok = (first_row + i) / a.group;
+                const Row mine = {tok, look_up.mask[i], FORMS ? sq.position(tok) : 0, 0.f};
+                float special[1][8] = {}, total = 0.f;
+                for (int k = 0; k < NW; ++k) total += ml[k][i].y;
+                for (int s = part.begin; s < part.end; ++s)
+                    if (all || (s + 1) * kStep > sq.len || s * kStep < part.all_from)
+                        add_unfit<HD, FMT, FORMS, 1, 8>(a, sq, look_up.at, mine, vr, s * kStep, c, g, d0, special);
+                if (row16 < 16 && 16 * r + row16 < live) put_special<HD, 8>(a, place, first_row + i, d0, total, special[0]);
+            }
+        }
+    }
     if (a.splits > 1 && a.arrived) {
         __shared__ int before;
         if (last_to_arrive(a, place, before))
@@ -725,7 +751,6 @@ struct alignas(16) Stage {
     static constexpr int KROW = 2 * HD + 16, VROW = 2 * HD + 32;
     char k[2][kBlockStep * KROW], v[2][kBlockStep * VROW];
     float scale[2][2][kBlockStep];
-    int unfit[2];                  // 1 + the step of this buffer that holds infinities or NaN among its values
 };
 
 // A row's 16-byte chunks (eight dimensions) in LDS: those of the second half of 128 dimensions change places in pairs.  The eight lanes that
@@ -765,6 +790,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     using S = Stage<HD>;
     __shared__ S lds;
     __shared__ Lookup<16 * NR * RW> look_up;
+    __shared__ int left_out;                                        // infinities or NaN were left out of the product
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
     const Place place(a);
     if (place.unit >= a.units) return;
@@ -797,7 +823,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
 
     Sums<HD> sum[NR];
-    bool careful = false, unfit = false;
+    bool careful = false;
 
     // ---- staging: requested a step ahead of the one that is written, which is a step ahead of the one that is used
     u32x4 kraw[PIECES], vraw[PIECES];
@@ -836,11 +862,11 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         if (!APART || 64 * wv >= APART)
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) put(lds.v[buf], S::VROW, vraw[i], tid + T * i - APART, look);
-        if (look && __any(odd)) lds.unfit[buf] = 1 + step;
+        if (look && __any(odd)) left_out = 1;
         if (SCALED && wv < 2)
             lds.scale[buf][wv][lane] = wv == 0 ? scale * to_score : at_least_small(scale);
     };
-    if (tid < 2) lds.unfit[tid] = 0;
+    if (tid == 0) left_out = 0;
     if (part.begin < part.end) {
         request(part.at(0));
         if (part.end * kBlockStep > sq.len) fill<FORMS, T>(a, sq, first_row, live, look_up);
@@ -858,7 +884,6 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         const int buf = i & 1, step = part.at(i), j0 = step * kBlockStep;
         const char *kb = lds.k[buf], *vb = lds.v[buf];
         const bool masked = masked_step(step);
-        if (FMT != CF_CACHE_INT8 && masked) unfit = __builtin_amdgcn_readfirstlane(lds.unfit[buf]) == 1 + step || unfit;
 #pragma unroll
         for (int h = 0; h < 2 / KG; ++h) {
             const int half = KG == 2 ? my_half : h;
@@ -890,18 +915,6 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         }
     }
 
-    if (FMT != CF_CACHE_INT8 && (unfit || not_finite(sum)))
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            f32x4 special[NJ] = {};
-            for (int i = 0; part.has(i); ++i)
-#pragma unroll 1
-                for (int h = 0; h < 2 / KG; ++h)
-                    put_unfit<HD, FMT, FORMS>(a, sq, look_up.at, row[r], vr, part.at(i) * kBlockStep + 32 * (KG == 2 ? my_half : h), c, g, special,
-                                              [&](int j, int rr) { return 16 * j + 4 * g + rr; });
-            take_over<HD>(special, sum[r].acc);
-        }
-
 #pragma unroll
     for (int r = 0; r < NR; ++r) sum[r].l = cf::lanes::sum_groups<16>(sum[r].l);
     if constexpr (KG == 2) {
@@ -928,7 +941,7 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
                 sum[r].mm = to;
                 sum[r].l = sum[r].l * mine + x.y * theirs;
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) sum[r].acc[j] = sum[r].acc[j] * for_sums(mine) + *reinterpret_cast<const f32x4 *>(other + i * STRIDE + 16 * j + 4 * g) * for_sums(theirs);
+                for (int j = 0; j < NJ; ++j) sum[r].acc[j] = sum[r].acc[j] * mine + *reinterpret_cast<const f32x4 *>(other + i * STRIDE + 16 * j + 4 * g) * theirs;
             }
     }
 #pragma unroll
@@ -959,6 +972,25 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
                 *reinterpret_cast<h4 *>(dst + 16 * j) = res;
             }
         }
+    }
+    if (FMT != CF_CACHE_INT8 && !my_half && my_rows < live) {
+        f32x4 odd = {0.f, 0.f, 0.f, 0.f};                           // NaN where a result is not finite
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) odd += sum[r].acc[j] * 0.f;
+        const bool all = __any((odd[0] + odd[1]) + (odd[2] + odd[3]) != 0.f);
+        if (part.begin < part.end && (all || __builtin_amdgcn_readfirstlane(left_out)))
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const int i = my_rows + 16 * r + c;
+                float special[NJ][4] = {};
+                for (int s = 2 * part.begin; s < 2 * part.end; ++s)
+                    if (all || masked_step(s / 2)) add_unfit<HD, FMT, FORMS, NJ, 4>(a, sq, look_up.at, row[r], vr, s * kStep, c, g, 4 * g, special);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    if (i < live) put_special<HD, 4>(a, place, first_row + i, 16 * j + 4 * g, sum[r].l, special[j]);
+            }
     }
     if (a.splits > 1 && a.arrived) {
         __shared__ int before;

@@ -193,3 +193,21 @@ def test_a_nan_scale_with_a_small_weight(fmt, T):
         c.vs[0, :, at] = np.nan
         assert np.isnan(c.run()).all(), at
         c.vs[0, :, at] = before
+
+
+@pytest.mark.parametrize("T", SIZES)
+def test_a_nan_score_beside_an_infinite_value(T):
+    """Every dimension of a token that sees a key of NaN is NaN, that of the infinity too; the others get the infinity."""
+    mask = np.zeros((T, T), bool)
+    mask[::2, 2] = True
+    c = _shaped("f16", T, mask=mask)
+    _put(c)
+    for splits in (1, 3):
+        c.tree.set_splits(splits)
+        clean = c.run()
+        keep = c.v[0, :, 10, 5].copy(), c.k[0, :, L + 2].copy()
+        c.v[0, :, 10, 5], c.k[0, :, L + 2] = np.inf, np.nan
+        got = c.run()
+        clean[..., 5] = np.inf
+        assert np.isnan(got[:, ::2]).all() and np.array_equal(got[:, 1::2], clean[:, 1::2])
+        c.v[0, :, 10, 5], c.k[0, :, L + 2] = keep
