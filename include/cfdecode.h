@@ -502,8 +502,10 @@ int cf_cache_keep(const cf_cache_config *cfg, int32_t batch, const cf_cache *cac
  * out [batch, tokens, n_q, head_dim] fp16, must not overlap q or the cache: rows of padding stay as they were; a token that sees
  * no key, or only keys with a score of minus infinity, gets zeros.  What a token does not see does not enter its result, whatever
  * it holds (NaN and infinities among it), to the bit.  A value that it sees and that is infinite or NaN makes that dimension of its
- * result infinite or NaN, however small the weight (NaN also where infinities of both signs meet).  Scores, softmax statistics and sums are fp32.  With the same row_len, row_tokens, max_len
- * and batch the same inputs give the same bits; otherwise the last bits may depend on how the cached rows are divided.
+ * result infinite or NaN, however small the weight (NaN also where infinities of both signs meet).  Scores, softmax statistics and sums are
+ * fp32; a weight enters the product with the values as fp16 (rounded by 2^-11 of itself, about as much as the result is, and by 2^-32 of the row's
+ * largest where it is smaller than 2^-21 of that).  With the same row_len, row_tokens, max_len and batch the same inputs give the same bits;
+ * otherwise the last bits may depend on how the cached rows are divided.
  *
  * cf_tree_create: a handle on the current device for calls of up to max_tokens tokens (1..256) with this score_cap (0: none) and
  *   window (0: none).  Allocates a workspace for partial results (synchronous).  CF_EINVAL also for a negative or non-finite

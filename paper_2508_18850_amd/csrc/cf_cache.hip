@@ -22,8 +22,9 @@ constexpr int kMaxKept = 256;      // tokens of a cf_cache_keep: their rows are 
 // takes 64 / (HD / 16) heads of one token at a time.  cos and sin of a token's HD / 2 angles are computed once, one angle to a thread,
 // and handed to all heads through LDS.
 // Arithmetic: angle, cos, sin and the rotation are fp64 and the result is rounded to fp16 once.  A fp32 rotation is off by 2^-23, which
-// moves one value in some thousands to the other fp16 neighbour, and through it one 8-bit code in 10^5; the fp64 one gives the
-// definition's bits; the vector units are idle beside it all the same (27.6 million instructions of 16384 wavefronts in 70 us).
+// moves one value in some thousands to the other fp16 neighbour, and through it one 8-bit code in 10^5; in fp64 the angle is off by some
+// 2^-51 of itself (a power, the product of two, the product with the position), at position 32768 by 2^-36, which moves one value in
+// 10^7; the vector units are idle beside it all the same (27.6 million instructions of 16384 wavefronts in 70 us).
 // Bound: memory.  Two prompts of 8192 and 6144 tokens, 32 + 2 x 8 heads of 128 dimensions, into int8: 324 MB in 70 us, 4.6 TB/s (a copy
 // reaches 4.8).  With few tokens the launch: one token 3.6 us on the GPU, so its heads are spread over more workgroups.
 struct AppendArgs {
@@ -257,7 +258,8 @@ int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, 
     a.rows = lengths_of(*draft);
     a.depth = draft->depth, a.depth_stride = draft->per_row ? draft->tokens : 0;
     a.nq = cfg->n_q_heads, a.nkv = cfg->n_kv_heads, a.max_seq = cfg->max_seq;
-    // theta_(8 i + j) = theta_(8 i) theta_j, off by 2^-51 of it: 16 powers on the host in place of 64 (one token 6.8 us a call, 7.2 with 64)
+    // theta_(8 i + j) = theta_(8 i) theta_j, off by 2^-51.4 of it at most (three half steps; a power alone by one): 16 powers on the host in place
+    // of 64 (one token 6.8 us a call, 7.2 with 64)
     double of_eight[8], in_eight[8];
     for (int i = 0; i < 8; ++i) {
         of_eight[i] = std::pow((double)cfg->rope_base, -16.0 * i / cfg->head_dim);

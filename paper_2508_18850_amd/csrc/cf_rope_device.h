@@ -44,8 +44,9 @@ __device__ __forceinline__ void rope_cos_sin(int pos, double inv_freq, float &co
     sin_out = (float)sv;
 }
 
-// cos and sin of pos * inv_freq in fp64, errors below 2^-51: the angle less the nearest multiple of pi / 2 (taken off in two parts),
-// the Taylor series of both up to a remainder of 2^-54 at pi / 4, and the quadrant.
+// cos and sin of the fp64 product pos * inv_freq, errors below 2^-51 for that angle (the product's own rounding comes on top, half a step:
+// 2^-39 where it is 2^14 to 2^15): the angle less the nearest multiple of pi / 2 (taken off in two parts), the Taylor series of both up to a remainder
+// of 2^-54 at pi / 4, and the quadrant.
 __device__ __forceinline__ void rope_cos_sin64(double pos, double inv_freq, double &cos_out, double &sin_out)
 {
     const double ang = pos * inv_freq;

@@ -561,8 +561,9 @@ __device__ __forceinline__ int join_lanes(int splits, int rows, int slots)
 
 // Few rows: reading the keys and values is the work.  Every wavefront has its own steps, so that no barrier holds up its loads: the next step's
 // keys are requested as soon as this one's are used, and its values.  The four wavefronts' sums are joined once, through LDS.
-// Bound: memory where the cache is long (one token over 32768 e4m3 rows, 64 heads: 69 MB in 14.2 us, 4.9 TB/s, then the join; a copy
-// reaches 4.8), the chain launch - lengths - queries - keys - values - sums where it is short (256 rows 5.7 us from launch to launch).
+// Bound: memory where the cache is long (one token over 32768 e4m3 rows, 64 heads: 69 MB in 14.0 us, 4.9 TB/s, then the join; a copy
+// reaches 4.8), the chain launch - lengths - queries - keys - values - sums where it is short (256 rows 5.9 us from launch to launch).  In
+// between a wavefront waits for its one step of loads: 64 tokens over 4096 e4m3 rows 41 % of its time, the matrix units busy 13 %.
 // Eight wavefronts to a workgroup were 5 % slower over 117 shapes: they start later and have more to join.
 // FORMS: the scores may be capped, biased or windowed.
 template <int HD, int FMT, int NR, bool FORMS>
@@ -773,10 +774,11 @@ __device__ __forceinline__ h8 transposed(const char *v, int first, int dim, int 
 // RW wavefronts with 16 NR rows each share the steps of a part; with KG = 2 there are two such groups, one for each half of a step, whose
 // sums are joined at the end.  (One group needs 1.15 us for a step of 128 dimensions when it has the compute unit for itself, most of it
 // the time from one instruction to the next that needs its result.)
-// Bound with many rows: the vector units.  Of the 2190 cycles that a wavefront with 32 rows takes for half a step (32 int8 keys, 128
-// dimensions), 590 are the scores' products, 1090 the weights (an exponential costs 8 cycles, and everything else of a weight as much
-// again), 510 the values' products; two such wavefronts share a SIMD and overlap in part.  16 x 64 tokens over 8192 int8 rows, 32 heads:
-// 138 GFLOP in 167 us, 0.83 PFLOP/s (a large fp16 product reaches 1.24), the matrix units busy a third of the time.
+// Bound with many rows: no unit is full.  16 x 64 tokens over 8192 int8 rows, 32 heads: 138 GFLOP in 165 to 176 us, 0.78 to 0.84 PFLOP/s (a
+// large fp16 product reaches 1.24); of the 337 thousand cycles that a compute unit is busy its matrix units are for 132 thousand, each SIMD
+// issues vector instructions for 173 thousand, and a wavefront waits for 34 % of its time.  Products, weights and products of a wavefront
+// follow each other (timed by phases, of 2190 cycles for half a step of 32 int8 keys by 32 rows, 128 dimensions, 590 were the scores'
+// products, 1090 the weights, 510 the values' products), and the two wavefronts of a SIMD overlap in part only.
 // Two groups in antiphase, steps of 128 keys and requests two steps ahead were 0 to 15 % slower.
 template <int HD, int FMT, int RW, int KG, int NR, bool FORMS>
 __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
