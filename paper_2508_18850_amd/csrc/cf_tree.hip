@@ -273,9 +273,10 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
 // A value that is infinite or NaN, and that a row sees, makes that dimension of its result infinite or NaN, however small the weight: the
 // weight of a key that a row sees is more than 0, though fp16 and fp32 may not hold it.  Products would give 0 times infinity there, and also
 // to the rows that do not see the key.  So steps in which some row does not see all keys leave such values out of the product, and where some
-// were left out, or results are not finite, the threads that wrote results look over the keys once more (behind their stores, where a jump
-// across this code costs nothing) and write the infinities and NaN that their rows see.
-
+// were left out, or results are not finite, the threads that wrote results look over the keys once more and write the infinities and NaN that
+// their rows see.  (Behind their stores: between the loop and the join the jump across this code cost a call of 7.3 us, one token over 512 e4m3
+// rows, up to 0.3.)
+//
 // The sums of those among P pieces of W adjacent values, from dimension d0 + 16 p on, of the 32 keys from j0 on, for one row of queries.
 template <int HD, int FMT, bool FORMS, int P, int W>
 __device__ __forceinline__ void add_unfit(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row &row, __amdgpu_buffer_rsrc_t vr, int j0, int c, int g,
@@ -311,6 +312,7 @@ __device__ __forceinline__ void add_unfit(const TreeArgs &a, const Sequence &sq,
             }
     }
 }
+
 // Where a workgroup works: workgroup i runs on die i mod 8, and the row blocks of a unit (a sequence's head and part), which read the same
 // keys and values, follow each other on one die.
 struct Place {
