@@ -417,19 +417,26 @@ int64_t cf_ffn_algorithmic_bytes(const cf_ffn_config *cfg, int32_t batch);
 
 /* ------------------------------------------------------------------------------------------------
  * Drafted tokens on a key/value cache: what a program that verifies several tokens per sequence at once (speculative
- * decoding), fills a cache from a prompt or holds it in 8 bits runs around its own projections.
+ * decoding), fills a cache from a prompt or holds it in 8 or 4 bits runs around its own projections (cf_linear_* below are such in 8 bits).
  *
  * The cache is that of cf_decode_block, [batch, n_kv_heads, max_seq, head_dim] for the keys and for the values, in one of
- * three formats:
+ * four formats:
  *   CF_CACHE_F16    fp16 (the tensors that cf_decode_block and cf_decode_layer take; no scales)
  *   CF_CACHE_E4M3   8-bit floats (OCP e4m3: 448 is the largest) and one fp32 scale for every cached row of a head,
  *   CF_CACHE_INT8   8-bit integers (-127..127)                  scales [batch, n_kv_heads, max_seq]; a value is code * scale
+ *   CF_CACHE_MXFP4  4-bit floats (OCP MXFP4: e2m1 codes of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign bit, 8) and a power of two for every 32
+ *                   adjacent values of a row (E8M0: one byte, 2^(byte - 127), 255: NaN); codes [.., max_seq, head_dim / 2] bytes, value 2 i in
+ *                   the low half of byte i, scales [batch, n_kv_heads, max_seq, head_dim / 32] bytes, given as the addresses k_scale, v_scale
  * A row (head_dim fp16 values) is held in 8 bits as  scale = top / Q  and  code = x * Q / top  rounded to the nearest code, ties to
  * even, where top is the row's largest magnitude and Q = 448 or 127; the code is the correctly rounded one.  A row of zeros has
  * scale 0 and codes 0; a row that holds an infinity or a NaN has scale NaN and codes 0, so that all of it reads back as NaN.
  * (Scales that another program writes have to be at least 0 as well, or NaN.)
+ * 32 values are held in 4 bits as  2^e, the smallest power of two with top <= 6 * 2^e that lies in 2^-23 .. 2^13  and  code = x / 2^e  rounded
+ * to the nearest of the values above, ties to the even code, magnitudes above 6 (of a top above 49152 only) to 6; a value that rounds to
+ * zero keeps its sign.  Every value that such a block stands for is an fp16 number.  32 values with an infinity or a NaN among them have
+ * scale byte 255 and codes 0, and all of them read back as NaN.  (Scale bytes that another program writes have to be 104..140 or 255.)
  */
-enum { CF_CACHE_F16 = 0, CF_CACHE_E4M3 = 1, CF_CACHE_INT8 = 2 };
+enum { CF_CACHE_F16 = 0, CF_CACHE_E4M3 = 1, CF_CACHE_INT8 = 2, CF_CACHE_MXFP4 = 4 };
 typedef struct cf_cache_config {
     int32_t n_q_heads, n_kv_heads;  /* n_q_heads % n_kv_heads == 0: query head i uses KV head i / (n_q_heads / n_kv_heads) */
     int32_t head_dim;               /* 64 or 128 */
@@ -438,8 +445,8 @@ typedef struct cf_cache_config {
     float   rope_base;
 } cf_cache_config;
 
-/* DEVICE pointers of a cache, k and v 16-byte aligned; the scales (4-byte aligned) are not read with CF_CACHE_F16 and may be NULL
- * then.  The four buffers must not overlap. */
+/* DEVICE pointers of a cache, k and v 16-byte aligned; the scales (4-byte aligned; bytes with CF_CACHE_MXFP4, whatever the type says) are not
+ * read with CF_CACHE_F16 and may be NULL then.  The four buffers must not overlap. */
 typedef struct cf_cache {
     void *k, *v;
     float *k_scale, *v_scale;
@@ -473,8 +480,12 @@ typedef struct cf_draft {
  *   and products in fp64, one rounding to fp16), q_out [batch, tokens, n_q, head_dim] fp16 receives the queries, the cache rows
  *   row_len[b] + t the keys and values.  Any number of tokens that the cache holds: a prompt, a tree, one token.  qkv, q_out and
  *   the cache must not overlap each other.
+ * cf_cache_append_normed: the same with every head of the queries and keys normalised before it is rotated,
+ *   y = x / sqrt(mean_j(x_j^2) + eps) * weight  over its head_dim values, with q_weight for queries and k_weight for keys (both DEVICE [head_dim]
+ *   fp16, 16-byte aligned, for all heads); norm and rotation in fp64, one rounding to fp16.  CF_EINVAL for eps < 0 or not finite, and for weights
+ *   that overlap q_out or the cache.  (With eps 0 a head of zeros becomes NaN.)
  * cf_cache_read: rows first .. first + rows - 1 of every head's slice as fp16, k_out and v_out [batch, n_kv, rows, head_dim]; 8-bit
- *   values are rounded once more, from the fp32 product code * scale.  rows 0 does nothing.  k_out, v_out and the cache must not
+ *   values are rounded once more, from the fp32 product code * scale (4-bit ones are fp16 numbers).  rows 0 does nothing.  k_out, v_out and the cache must not
  *   overlap each other.
  * cf_cache_keep: after verification, row row_len[b] + i of every head's slice becomes what row row_len[b] + kept[b][i] was, for
  *   i < n_kept[b] (keys, values and scales; all rows are read before one is written); the rows behind stay as they were.  kept: DEVICE [batch,
@@ -484,6 +495,8 @@ typedef struct cf_draft {
  */
 int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, const cf_cache *cache, const cf_draft *draft,
                     void *q_out, void *stream);
+int cf_cache_append_normed(const cf_cache_config *cfg, int32_t batch, const void *qkv, const void *q_weight, const void *k_weight, float eps,
+                           const cf_cache *cache, const cf_draft *draft, void *q_out, void *stream);
 int cf_cache_read(const cf_cache_config *cfg, int32_t batch, const cf_cache *cache, int32_t first, int32_t rows, void *k_out,
                   void *v_out, void *stream);
 int cf_cache_keep(const cf_cache_config *cfg, int32_t batch, const cf_cache *cache, const cf_draft *draft, const int32_t *kept,
@@ -528,6 +541,42 @@ int cf_tree_attend(cf_tree t, int32_t batch, const void *q, const cf_cache *cach
                    void *out, void *stream);
 int cf_tree_set_splits(cf_tree t, int32_t max_splits);
 int64_t cf_tree_algorithmic_bytes(const cf_tree_config *cfg, int32_t batch, int32_t tokens, int32_t len);
+
+/* ------------------------------------------------------------------------------------------------
+ * Projections in 8-bit integers: rows of fp16 as codes with one scale for each row (a token, or an output channel of the weights), and the product
+ * of such rows with such weights.  For any number of rows: one token, drafted tokens, prompts.
+ *
+ *   code[m][k] = x[m][k] * 127 / top_m rounded to nearest, ties to even;  scale[m] = top_m / 127;  top_m: the row's largest magnitude
+ *   out[m][n]  = (sum_k x[m][k] W[n][k]) * x_scale[m] * w_scale[n]
+ *
+ * The sum is exact (32-bit integers); it is converted to fp32 and multiplied by the two scales in this order, each step rounded, and rounded to fp16.
+ * All pointers are DEVICE pointers, 16-byte aligned (scales: 4), dense and row-major; the caller owns them.
+ *
+ * cf_linear_quantize: x [rows, n] fp16 read, codes [rows, n] and scale [rows] written; the codes are those of CF_CACHE_INT8, correctly rounded: a
+ *   row of zeros has scale 0 and codes 0, a row that holds an infinity or a NaN scale NaN and codes 0 (and all of its product is NaN).
+ *   CF_EINVAL: rows below 0, n not a positive multiple of 16, null or misaligned pointers, buffers that overlap; CF_EUNSUPPORTED: more than 2^23
+ *   rows.  rows 0 does nothing.
+ * cf_linear_create: a handle on the current device for products of up to max_rows rows with weights of this shape (synchronous).
+ *   CF_EINVAL for n_in not a positive multiple of 16, n_out not a positive multiple of 8, max_rows below 1; CF_EUNSUPPORTED for n_in above 131056,
+ *   weights of 2 GiB or more, max_rows above 2^23.
+ * cf_linear_forward: x [rows, n_in], x_scale [rows], W [n_out, n_in] (row n: the weights into output n), w_scale [n_out] read; out [rows,
+ *   n_out] fp16 fully overwritten.  Codes may have any value from -128 on.  CF_EINVAL: null or misaligned pointers, rows outside
+ *   1..max_rows, out overlapping an input, another current device than the handle's.
+ * The same inputs give the same bits.  cf_linear_quantize and cf_linear_forward are asynchronous on `stream`, allocate nothing and can be
+ * captured and replayed.  A handle must not be used from two streams at the same time, nor two captured graphs with calls on one handle replayed
+ * at the same time.
+ */
+typedef struct cf_linear_config {
+    int32_t n_in, n_out, max_rows;
+} cf_linear_config;
+typedef struct cf_linear_s *cf_linear;
+int cf_linear_quantize(int32_t rows, int32_t n, const void *x, int8_t *codes, float *scale, void *stream);
+int cf_linear_create(const cf_linear_config *cfg, cf_linear *out);
+int cf_linear_destroy(cf_linear t);
+int cf_linear_forward(cf_linear t, int32_t rows, const int8_t *x, const float *x_scale, const int8_t *W, const float *w_scale, void *out,
+                      void *stream);
+/* HBM bytes that a product cannot do without (codes, scales and weights once, out). */
+int64_t cf_linear_algorithmic_bytes(const cf_linear_config *cfg, int32_t rows);
 
 #ifdef __cplusplus
 }

@@ -26,8 +26,9 @@ EXPORTED_SYMBOLS = ("cf_create", "cf_destroy", "cf_decode_block", "cf_decode_blo
                     "cf_splithead_status", "cf_splithead_set_spin_limit",
                     "cf_ffn_create", "cf_ffn_destroy", "cf_ffn_decode", "cf_ffn_status", "cf_ffn_set_spin_limit",
                     "cf_ffn_algorithmic_bytes",
-                    "cf_cache_append", "cf_cache_read", "cf_cache_keep",
-                    "cf_tree_create", "cf_tree_destroy", "cf_tree_attend", "cf_tree_set_splits", "cf_tree_algorithmic_bytes")
+                    "cf_cache_append", "cf_cache_append_normed", "cf_cache_read", "cf_cache_keep",
+                    "cf_tree_create", "cf_tree_destroy", "cf_tree_attend", "cf_tree_set_splits", "cf_tree_algorithmic_bytes",
+                    "cf_linear_quantize", "cf_linear_create", "cf_linear_destroy", "cf_linear_forward", "cf_linear_algorithmic_bytes")
 
 CF_FLAG_DEBUG_EXPORT = 1
 
@@ -73,7 +74,11 @@ class TreeConfig(ctypes.Structure):
     _fields_ = [("cache", CacheConfig), ("max_tokens", ctypes.c_int32), ("score_cap", ctypes.c_float), ("window", ctypes.c_int32)]
 
 
-CACHE_F16, CACHE_E4M3, CACHE_INT8 = 0, 1, 2
+class LinearConfig(ctypes.Structure):
+    _fields_ = [("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32), ("max_rows", ctypes.c_int32)]
+
+
+CACHE_F16, CACHE_E4M3, CACHE_INT8, CACHE_MXFP4 = 0, 1, 2, 4
 
 
 class CfError(RuntimeError):
@@ -153,6 +158,7 @@ def load_library():
             getattr(lib, name).restype = ctypes.c_int
         cfg_p, cache_p, draft_p = ctypes.POINTER(CacheConfig), ctypes.POINTER(Cache), ctypes.POINTER(Draft)
         lib.cf_cache_append.argtypes = [cfg_p, i32, vp, cache_p, draft_p, vp, vp]
+        lib.cf_cache_append_normed.argtypes = [cfg_p, i32, vp, vp, vp, ctypes.c_float, cache_p, draft_p, vp, vp]
         lib.cf_cache_read.argtypes = [cfg_p, i32, cache_p, i32, i32, vp, vp, vp]
         lib.cf_cache_keep.argtypes = [cfg_p, i32, cache_p, draft_p, vp, vp, vp, vp]
         lib.cf_tree_create.argtypes = [ctypes.POINTER(TreeConfig), ctypes.POINTER(vp)]
@@ -161,8 +167,14 @@ def load_library():
         lib.cf_tree_set_splits.argtypes = [vp, i32]
         lib.cf_tree_algorithmic_bytes.argtypes = [ctypes.POINTER(TreeConfig), i32, i32, i32]
         lib.cf_tree_algorithmic_bytes.restype = ctypes.c_int64
-        for name in ("cf_cache_append", "cf_cache_read", "cf_cache_keep", "cf_tree_create", "cf_tree_destroy", "cf_tree_attend",
-                     "cf_tree_set_splits"):
+        lib.cf_linear_quantize.argtypes = [i32, i32, vp, vp, vp, vp]
+        lib.cf_linear_create.argtypes = [ctypes.POINTER(LinearConfig), ctypes.POINTER(vp)]
+        lib.cf_linear_destroy.argtypes = [vp]
+        lib.cf_linear_forward.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
+        lib.cf_linear_algorithmic_bytes.argtypes = [ctypes.POINTER(LinearConfig), i32]
+        lib.cf_linear_algorithmic_bytes.restype = ctypes.c_int64
+        for name in ("cf_cache_append", "cf_cache_append_normed", "cf_cache_read", "cf_cache_keep", "cf_tree_create", "cf_tree_destroy",
+                     "cf_tree_attend", "cf_tree_set_splits", "cf_linear_quantize", "cf_linear_create", "cf_linear_destroy", "cf_linear_forward"):
             getattr(lib, name).restype = ctypes.c_int
         lib.cf_decode_stack.argtypes = [vp, i32, i32, vp, ctypes.POINTER(vp), ctypes.c_float, i32, i32, ctypes.POINTER(vp),
                                         ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(vp), i32, vp, vp]
@@ -480,7 +492,8 @@ class SplitHeadBlock:
 
 
 def cache_pointers(k, v, k_scale=0, v_scale=0) -> Cache:
-    """The buffers of a key/value cache (cf_cache) from their device addresses; the scales are needed with 8-bit formats."""
+    """The buffers of a key/value cache (cf_cache) from their device addresses; the scales are needed with 8-bit and 4-bit
+    formats."""
     return Cache(k or None, v or None, k_scale or None, v_scale or None)
 
 
@@ -490,7 +503,7 @@ def draft(tokens, max_len, row_len=0, row_tokens=0, depth=0, tree=0, per_row=Fal
 
 
 class KvCache:
-    """Calls on a key/value cache in fp16 or 8 bits (cf_cache_*).  Tensors are raw device addresses; `cache` and `draft` come
+    """Calls on a key/value cache in fp16, 8 or 4 bits (cf_cache_*).  Tensors are raw device addresses; `cache` and `draft` come
     from cache_pointers() and draft()."""
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, format, rope_base):
@@ -508,6 +521,14 @@ class KvCache:
 
     def append_rc(self, batch, qkv, cache, draft, q_out, stream=0) -> int:
         return int(self._lib.cf_cache_append(self.cfg, batch, qkv, cache, draft, q_out, stream))
+
+    def append_normed(self, batch, qkv, q_weight, k_weight, eps, cache, draft, q_out, stream=0):
+        rc = self._lib.cf_cache_append_normed(self.cfg, batch, qkv, q_weight, k_weight, eps, cache, draft, q_out, stream)
+        if rc != 0:
+            self._check(rc)
+
+    def append_normed_rc(self, batch, qkv, q_weight, k_weight, eps, cache, draft, q_out, stream=0) -> int:
+        return int(self._lib.cf_cache_append_normed(self.cfg, batch, qkv, q_weight, k_weight, eps, cache, draft, q_out, stream))
 
     def read(self, batch, cache, first, rows, k_out, v_out, stream=0):
         rc = self._lib.cf_cache_read(self.cfg, batch, cache, first, rows, k_out, v_out, stream)
@@ -557,6 +578,53 @@ class TreeAttention:
     def close(self):
         if self._h:
             self._lib.cf_tree_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def quantize_rows(rows, n, x, codes, scale, stream=0):
+    """fp16 rows [rows, n] as int8 codes and one fp32 scale a row (cf_linear_quantize).  Raw device addresses."""
+    rc = quantize_rows_rc(rows, n, x, codes, scale, stream)
+    if rc != 0:
+        raise CfError(rc, load_library().cf_strerror(rc).decode())
+
+
+def quantize_rows_rc(rows, n, x, codes, scale, stream=0) -> int:
+    return int(load_library().cf_linear_quantize(rows, n, x, codes, scale, stream))
+
+
+class Int8Linear:
+    """Handle of the product of int8 rows with int8 weights (cf_linear_*).  Tensors are raw device addresses."""
+
+    def __init__(self, n_in, n_out, max_rows):
+        self._lib = load_library()
+        self.cfg = LinearConfig(n_in, n_out, max_rows)
+        self._h = ctypes.c_void_p()
+        self._check(self._lib.cf_linear_create(ctypes.byref(self.cfg), ctypes.byref(self._h)))
+
+    def _check(self, rc):
+        if rc != 0:
+            raise CfError(rc, self._lib.cf_strerror(rc).decode())
+
+    def forward(self, rows, x, x_scale, w, w_scale, out, stream=0):
+        rc = self._lib.cf_linear_forward(self._h, rows, x, x_scale, w, w_scale, out, stream)
+        if rc != 0:
+            self._check(rc)
+
+    def forward_rc(self, rows, x, x_scale, w, w_scale, out, stream=0) -> int:
+        return int(self._lib.cf_linear_forward(self._h, rows, x, x_scale, w, w_scale, out, stream))
+
+    def algorithmic_bytes(self, rows) -> int:
+        return int(self._lib.cf_linear_algorithmic_bytes(ctypes.byref(self.cfg), rows))
+
+    def close(self):
+        if self._h:
+            self._lib.cf_linear_destroy(self._h)
             self._h = ctypes.c_void_p()
 
     def __del__(self):

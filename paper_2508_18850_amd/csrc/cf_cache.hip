@@ -1,4 +1,4 @@
-// A key/value cache in fp16 or 8 bits: written with the rotated keys and the values of new tokens, read back as fp16, and its rows of
+// A key/value cache in fp16, 8 bits or 4 bits: written with the rotated keys and the values of new tokens, read back as fp16, and its rows of
 // accepted tokens moved together (cf_cache_* in include/cfdecode.h).  Three kernels without waits between workgroups.
 #include "../../include/cfdecode.h"
 #include "cf_cache_device.h"
@@ -31,7 +31,9 @@ struct AppendArgs {
     const uint16_t *qkv;
     uint16_t *q_out;
     char *k, *v;
-    float *k_scale, *v_scale;
+    float *k_scale, *v_scale;      // of the 4-bit format: bytes
+    const uint16_t *q_weight, *k_weight;   // with norms
+    double eps;
     Lengths rows;
     const int32_t *depth;
     int depth_stride;              // depths of a batch row: 0 where all share them
@@ -59,7 +61,44 @@ __device__ __forceinline__ uint32_t row_top(uint32_t t)      // largest of the H
     return HD == 64 ? t : max(t, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0x141, 0xF, 0xF, true));   // 7 - lane
 }
 
-template <int HD, int FMT>
+// of the four lanes that hold a block of the 4-bit format
+__device__ __forceinline__ uint32_t block_top(uint32_t t)
+{
+    t = max(t, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0xB1, 0xF, 0xF, true));
+    return max(t, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0x4E, 0xF, 0xF, true));
+}
+
+template <int CTRL>
+__device__ __forceinline__ double moved(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// 1 / sqrt(mean of the squares of a row + eps), in fp64: the squares of fp16 values are exact, their sum is off by HD half steps of 2^-53, and two
+// Newton steps take the approximation of v_rsq_f64 (2^-26 or better) to 2^-51.
+template <int HD>
+__device__ __forceinline__ double row_norm(const h8 &lo, const h8 &hi, double eps)
+{
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const double x = (double)(float)lo[j], y = (double)(float)hi[j];
+        s = fma(x, x, s);
+        s = fma(y, y, s);
+    }
+    s += moved<0xB1>(s);
+    s += moved<0x4E>(s);
+    if constexpr (HD == 128) s += moved<0x141>(s);
+    const double m = s * (1.0 / HD) + eps;
+    double r = __builtin_amdgcn_rsq(m);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = fma(0.5 * r, fma(-m * r, r, 1.0), r);
+    return m == (double)INFINITY ? 0.0 : r;
+}
+
+template <int HD, int FMT, bool NORM>
 __global__ __launch_bounds__(NT) void cache_append(const AppendArgs a)
 {
     constexpr int LPR = HD / 16, RPW = 64 / LPR, HALF = HD / 2;
@@ -88,10 +127,18 @@ __global__ __launch_bounds__(NT) void cache_append(const AppendArgs a)
         const uint16_t *src = a.qkv + (((size_t)b * a.rows.tokens + t) * H + head) * HD + 8 * li;
         h8 lo = *reinterpret_cast<const h8 *>(src), hi = *reinterpret_cast<const h8 *>(src + HALF);
         if (head < a.nq + a.nkv) {
+            h8 wlo, whi;
+            double r = 1.0;
+            if constexpr (NORM) {
+                const uint16_t *w = (head < a.nq ? a.q_weight : a.k_weight) + 8 * li;
+                wlo = *reinterpret_cast<const h8 *>(w), whi = *reinterpret_cast<const h8 *>(w + HALF);
+                r = row_norm<HD>(lo, hi, a.eps);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const double2 cs = turn[slot][8 * li + j];
-                const double x = (double)(float)lo[j], y = (double)(float)hi[j];
+                double x = (double)(float)lo[j], y = (double)(float)hi[j];
+                if constexpr (NORM) x *= (double)(float)wlo[j] * r, y *= (double)(float)whi[j] * r;
                 lo[j] = half_once(x * cs.x - y * cs.y);
                 hi[j] = half_once(y * cs.x + x * cs.y);
             }
@@ -104,10 +151,18 @@ __global__ __launch_bounds__(NT) void cache_append(const AppendArgs a)
         }
         const bool key = head < a.nq + a.nkv;
         const size_t row = ((size_t)b * a.nkv + (head - a.nq - (key ? 0 : a.nkv))) * a.max_seq + len + t;
-        char *dst = (key ? a.k : a.v) + (row * HD + 8 * li) * kValueBytes<FMT>;
+        char *dst = (key ? a.k : a.v) + row * bytes_of<FMT>(HD) + bytes_of<FMT>(8) * li;
         if constexpr (FMT == CF_CACHE_F16) {
             *reinterpret_cast<h8 *>(dst) = lo;
             *reinterpret_cast<h8 *>(dst + 2 * HALF) = hi;
+        } else if constexpr (FMT == CF_CACHE_MXFP4) {
+            const uint32_t slo = block_scale(block_top(top_bits(lo))), shi = block_scale(block_top(top_bits(hi)));
+            *reinterpret_cast<uint32_t *>(dst) = block_codes(lo, slo);
+            *reinterpret_cast<uint32_t *>(dst + HALF / 2) = block_codes(hi, shi);
+            if (li % 4 == 0) {
+                uint8_t *scale = reinterpret_cast<uint8_t *>(key ? a.k_scale : a.v_scale) + row * (HD / kBlock) + li / 4;
+                scale[0] = (uint8_t)slo, scale[HALF / kBlock] = (uint8_t)shi;
+            }
         } else {
             const Encoder<FMT> enc(row_top<HD>(max(top_bits(lo), top_bits(hi))));
             *reinterpret_cast<u32x2 *>(dst) = enc.codes(lo);
@@ -135,8 +190,8 @@ __global__ __launch_bounds__(NT) void cache_read(const ReadArgs a)
 {
     const bool key = blockIdx.z == 0;
     const size_t slice = (size_t)blockIdx.y * a.max_seq + a.first;
-    const char *src = (key ? a.k : a.v) + slice * HD * kValueBytes<FMT>;
-    const float *scale = (key ? a.k_scale : a.v_scale) + (FMT == CF_CACHE_F16 ? 0 : slice);
+    const char *src = (key ? a.k : a.v) + slice * bytes_of<FMT>(HD);
+    const float *scale = (key ? a.k_scale : a.v_scale) + (FMT == CF_CACHE_F16 || FMT == CF_CACHE_MXFP4 ? 0 : slice);
     uint16_t *dst = (key ? a.k_out : a.v_out) + (size_t)blockIdx.y * a.rows * HD;
     const uint32_t pieces = (uint32_t)a.rows * (HD / 16), at = blockIdx.x * (NT * kReadPieces) + threadIdx.x;
     if constexpr (FMT == CF_CACHE_F16) {
@@ -149,6 +204,21 @@ __global__ __launch_bounds__(NT) void cache_read(const ReadArgs a)
         for (int i = 0; i < kReadPieces; ++i)
             if (at + NT * i < pieces)
                 for (int w = 0; w < 2; ++w) *reinterpret_cast<u32x4 *>(dst + (size_t)(at + NT * i) * 16 + 8 * w) = x[i][w];
+    } else if constexpr (FMT == CF_CACHE_MXFP4) {
+        const uint8_t *power = reinterpret_cast<const uint8_t *>(scale) + slice * (HD / kBlock);
+        u32x2 x[kReadPieces];
+        uint32_t s[kReadPieces];
+#pragma unroll
+        for (int i = 0; i < kReadPieces; ++i)
+            if (at + NT * i < pieces) {
+                x[i] = *reinterpret_cast<const u32x2 *>(src + (size_t)(at + NT * i) * 8);
+                s[i] = power[(at + NT * i) / 2];
+            }
+#pragma unroll
+        for (int i = 0; i < kReadPieces; ++i)
+            if (at + NT * i < pieces)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) *reinterpret_cast<u32x4 *>(dst + (size_t)(at + NT * i) * 16 + 8 * w) = block_values(x[i][w], scale_of_byte(s[i]));
     } else {
         u32x4 x[kReadPieces];
         float s[kReadPieces];
@@ -181,11 +251,12 @@ __global__ __launch_bounds__(NT) void cache_read(const ReadArgs a)
 
 struct KeepArgs {
     char *k, *v;
-    float *k_scale, *v_scale;
+    char *k_scale, *v_scale;
     Lengths rows;
     const int32_t *kept, *n_kept;
     int32_t *new_len;
     int nkv, max_seq, row_bytes;
+    int scale_bytes;               // of a row's scales: 0, 2 or 4
 };
 
 // One workgroup per head's slice: its kept rows into LDS, a barrier, and out to their places (a place may be another row's source).
@@ -200,17 +271,21 @@ __global__ __launch_bounds__(NT) void cache_keep(const KeepArgs a)
     if (a.new_len && tid == 0 && key && blockIdx.y % a.nkv == 0) a.new_len[b] = len + moved;
     const size_t first = (size_t)blockIdx.y * a.max_seq + len;
     char *rows = (key ? a.k : a.v) + first * a.row_bytes;
-    float *scale = key ? a.k_scale : a.v_scale;
+    char *scale = (key ? a.k_scale : a.v_scale) + first * a.scale_bytes;
     const int32_t *kept = a.kept + (size_t)b * a.rows.tokens;
-    const int per = a.row_bytes / 16;                              // 4, 8 or 16 pieces of a row
+    const int per = a.row_bytes / 16;                              // 2, 4, 8 or 16 pieces of a row
     for (int e = tid; e < moved * per; e += NT) {
         const int from = min(max(kept[e / per], 0), n - 1);
         *reinterpret_cast<u32x4 *>(held + 16 * e) = *reinterpret_cast<const u32x4 *>(rows + (size_t)from * a.row_bytes + 16 * (e % per));
     }
-    const float own_scale = scale && tid < moved ? scale[first + min(max(kept[tid], 0), n - 1)] : 0.f;
+    const int mine = tid < moved ? min(max(kept[tid], 0), n - 1) : 0;
+    uint32_t own_scale = 0;
+    if (tid < moved && a.scale_bytes == 4) own_scale = reinterpret_cast<const uint32_t *>(scale)[mine];
+    if (tid < moved && a.scale_bytes == 2) own_scale = reinterpret_cast<const uint16_t *>(scale)[mine];
     __syncthreads();
     for (int e = tid; e < moved * per; e += NT) *reinterpret_cast<u32x4 *>(rows + 16 * (size_t)e) = *reinterpret_cast<const u32x4 *>(held + 16 * e);
-    if (scale && tid < moved) scale[first + tid] = own_scale;
+    if (tid < moved && a.scale_bytes == 4) reinterpret_cast<uint32_t *>(scale)[tid] = own_scale;
+    if (tid < moved && a.scale_bytes == 2) reinterpret_cast<uint16_t *>(scale)[tid] = (uint16_t)own_scale;
 }
 static_assert(kMaxKept <= NT, "a thread per scale");
 
@@ -218,25 +293,30 @@ static_assert(kMaxKept <= NT, "a thread per scale");
 
 template <typename Args>
 using Kernel = void (*)(const Args);
-Kernel<AppendArgs> pick_append(int hd, int fmt)
+template <int HD, bool NORM>
+Kernel<AppendArgs> pick_append_of(int fmt)
 {
-    if (hd == 64) return fmt == CF_CACHE_F16 ? cache_append<64, CF_CACHE_F16> : fmt == CF_CACHE_E4M3 ? cache_append<64, CF_CACHE_E4M3> : cache_append<64, CF_CACHE_INT8>;
-    return fmt == CF_CACHE_F16 ? cache_append<128, CF_CACHE_F16> : fmt == CF_CACHE_E4M3 ? cache_append<128, CF_CACHE_E4M3> : cache_append<128, CF_CACHE_INT8>;
+    return fmt == CF_CACHE_F16 ? cache_append<HD, CF_CACHE_F16, NORM> : fmt == CF_CACHE_E4M3 ? cache_append<HD, CF_CACHE_E4M3, NORM> :
+           fmt == CF_CACHE_INT8 ? cache_append<HD, CF_CACHE_INT8, NORM> : cache_append<HD, CF_CACHE_MXFP4, NORM>;
 }
-Kernel<ReadArgs> pick_read(int hd, int fmt)
+Kernel<AppendArgs> pick_append(int hd, int fmt, bool norm)
 {
-    if (hd == 64) return fmt == CF_CACHE_F16 ? cache_read<64, CF_CACHE_F16> : fmt == CF_CACHE_E4M3 ? cache_read<64, CF_CACHE_E4M3> : cache_read<64, CF_CACHE_INT8>;
-    return fmt == CF_CACHE_F16 ? cache_read<128, CF_CACHE_F16> : fmt == CF_CACHE_E4M3 ? cache_read<128, CF_CACHE_E4M3> : cache_read<128, CF_CACHE_INT8>;
+    if (hd == 64) return norm ? pick_append_of<64, true>(fmt) : pick_append_of<64, false>(fmt);
+    return norm ? pick_append_of<128, true>(fmt) : pick_append_of<128, false>(fmt);
 }
+template <int HD>
+Kernel<ReadArgs> pick_read_of(int fmt)
+{
+    return fmt == CF_CACHE_F16 ? cache_read<HD, CF_CACHE_F16> : fmt == CF_CACHE_E4M3 ? cache_read<HD, CF_CACHE_E4M3> :
+           fmt == CF_CACHE_INT8 ? cache_read<HD, CF_CACHE_INT8> : cache_read<HD, CF_CACHE_MXFP4>;
+}
+Kernel<ReadArgs> pick_read(int hd, int fmt) { return hd == 64 ? pick_read_of<64>(fmt) : pick_read_of<128>(fmt); }
 
 int launched() { return hipGetLastError() == hipSuccess ? CF_OK : CF_EHIP; }
 
-}  // namespace
-
-extern "C" {
-
-int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, const cf_cache *cache, const cf_draft *draft,
-                    void *q_out, void *stream)
+// cf_cache_append, and cf_cache_append_normed where there are weights (norm).
+int append(const cf_cache_config *cfg, int32_t batch, const void *qkv, bool norm, const void *q_weight, const void *k_weight, float eps,
+           const cf_cache *cache, const cf_draft *draft, void *q_out, void *stream)
 {
     if (!cfg) return CF_EINVAL;
     int rc = check_config(*cfg);
@@ -244,10 +324,15 @@ int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, 
     if (rc == CF_OK) rc = check_draft(*cfg, draft);
     if (rc != CF_OK) return rc;
     if (!qkv || !q_out || !aligned(qkv, 16) || !aligned(q_out, 16)) return CF_EINVAL;
+    if (norm && (!q_weight || !k_weight || !aligned(q_weight, 16) || !aligned(k_weight, 16) || !(eps >= 0.f) || !(eps <= 3.402823466e38f))) return CF_EINVAL;
     const size_t head_values = (size_t)batch * draft->tokens * cfg->head_dim;
     const size_t qkv_bytes = 2 * head_values * (cfg->n_q_heads + 2 * (size_t)cfg->n_kv_heads), q_bytes = 2 * head_values * cfg->n_q_heads;
     if (overlap(qkv, qkv_bytes, q_out, q_bytes) || in_cache(*cfg, *cache, batch, qkv, qkv_bytes) ||
         in_cache(*cfg, *cache, batch, q_out, q_bytes) || tangled(*cfg, *cache, batch))
+        return CF_EINVAL;
+    const size_t weight_bytes = 2 * (size_t)cfg->head_dim;
+    if (norm && (overlap(q_weight, weight_bytes, q_out, q_bytes) || overlap(k_weight, weight_bytes, q_out, q_bytes) ||
+                 in_cache(*cfg, *cache, batch, q_weight, weight_bytes) || in_cache(*cfg, *cache, batch, k_weight, weight_bytes)))
         return CF_EINVAL;
     AppendArgs a;
     std::memset(&a, 0, sizeof a);
@@ -255,6 +340,7 @@ int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, 
     a.q_out = static_cast<uint16_t *>(q_out);
     a.k = static_cast<char *>(cache->k), a.v = static_cast<char *>(cache->v);
     a.k_scale = cache->k_scale, a.v_scale = cache->v_scale;
+    a.q_weight = static_cast<const uint16_t *>(q_weight), a.k_weight = static_cast<const uint16_t *>(k_weight), a.eps = eps;
     a.rows = lengths_of(*draft);
     a.depth = draft->depth, a.depth_stride = draft->per_row ? draft->tokens : 0;
     a.nq = cfg->n_q_heads, a.nkv = cfg->n_kv_heads, a.max_seq = cfg->max_seq;
@@ -270,9 +356,25 @@ int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, 
     const int heads = a.nq + 2 * a.nkv, groups = (heads * cfg->head_dim / 16 + 63) / 64;
     a.nt = (long long)batch * draft->tokens >= 2048 ? 4 : 1;
     const int chunks = a.nt == 4 ? 1 : (groups + NW - 1) / NW;
-    hipLaunchKernelGGL(pick_append(cfg->head_dim, cfg->format), dim3((draft->tokens + a.nt - 1) / a.nt, chunks, batch), dim3(NT), 0,
+    hipLaunchKernelGGL(pick_append(cfg->head_dim, cfg->format, norm), dim3((draft->tokens + a.nt - 1) / a.nt, chunks, batch), dim3(NT), 0,
                        static_cast<hipStream_t>(stream), a);
     return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int cf_cache_append(const cf_cache_config *cfg, int32_t batch, const void *qkv, const cf_cache *cache, const cf_draft *draft,
+                    void *q_out, void *stream)
+{
+    return append(cfg, batch, qkv, false, nullptr, nullptr, 0.f, cache, draft, q_out, stream);
+}
+
+int cf_cache_append_normed(const cf_cache_config *cfg, int32_t batch, const void *qkv, const void *q_weight, const void *k_weight, float eps,
+                           const cf_cache *cache, const cf_draft *draft, void *q_out, void *stream)
+{
+    return append(cfg, batch, qkv, true, q_weight, k_weight, eps, cache, draft, q_out, stream);
 }
 
 int cf_cache_read(const cf_cache_config *cfg, int32_t batch, const cf_cache *cache, int32_t first, int32_t rows, void *k_out,
@@ -320,11 +422,12 @@ int cf_cache_keep(const cf_cache_config *cfg, int32_t batch, const cf_cache *cac
     KeepArgs a;
     std::memset(&a, 0, sizeof a);
     a.k = static_cast<char *>(cache->k), a.v = static_cast<char *>(cache->v);
-    if (cfg->format != CF_CACHE_F16) a.k_scale = cache->k_scale, a.v_scale = cache->v_scale;
+    a.k_scale = reinterpret_cast<char *>(cache->k_scale), a.v_scale = reinterpret_cast<char *>(cache->v_scale);
+    a.scale_bytes = row_scale_bytes(*cfg);
     a.rows = lengths_of(*draft);
     a.kept = kept, a.n_kept = n_kept, a.new_len = new_len;
     a.nkv = cfg->n_kv_heads, a.max_seq = cfg->max_seq;
-    a.row_bytes = cfg->head_dim * (cfg->format == CF_CACHE_F16 ? 2 : 1);
+    a.row_bytes = row_bytes(*cfg);
     hipLaunchKernelGGL(cache_keep, dim3(1, batch * cfg->n_kv_heads, 2), dim3(NT), (size_t)draft->tokens * a.row_bytes,
                        static_cast<hipStream_t>(stream), a);
     return launched();

@@ -1,5 +1,5 @@
 // What the kernels on a key/value cache in one of the formats of cf_cache_config share: lengths of the batch rows, encoding and
-// decoding of 8-bit rows, the checks of the arguments.
+// decoding of 8-bit and 4-bit rows, the checks of the arguments.
 #ifndef CF_CACHE_DEVICE_H
 #define CF_CACHE_DEVICE_H
 
@@ -12,6 +12,7 @@ namespace cf {
 namespace cache {
 
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -19,7 +20,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int FMT>
 constexpr float kLargest = FMT == CF_CACHE_INT8 ? 127.f : 448.f;
 template <int FMT>
-constexpr int kValueBytes = FMT == CF_CACHE_F16 ? 2 : 1;
+constexpr int kValueBytes = FMT == CF_CACHE_F16 ? 2 : 1;          // (not of the 4-bit format)
+// bytes of `values` adjacent values
+template <int FMT>
+constexpr int bytes_of(int values) { return FMT == CF_CACHE_F16 ? 2 * values : FMT == CF_CACHE_MXFP4 ? values / 2 : values; }
+constexpr int kBlock = 32;           // values under one scale of the 4-bit format
 
 // The batch rows' lengths (cf_draft without its masks).
 struct Lengths {
@@ -41,7 +46,7 @@ inline bool overlap(const void *p, size_t p_bytes, const void *q, size_t q_bytes
 inline int check_config(const cf_cache_config &c)
 {
     if (c.n_q_heads < 1 || c.n_kv_heads < 1 || c.n_q_heads % c.n_kv_heads || c.max_batch < 1 || c.max_seq < 1 ||
-        (c.format != CF_CACHE_F16 && c.format != CF_CACHE_E4M3 && c.format != CF_CACHE_INT8) || !(c.rope_base > 1.0f) ||
+        (c.format != CF_CACHE_F16 && c.format != CF_CACHE_E4M3 && c.format != CF_CACHE_INT8 && c.format != CF_CACHE_MXFP4) || !(c.rope_base > 1.0f) ||
         !(c.rope_base <= 3.402823466e38f))
         return CF_EINVAL;
     if (c.head_dim != 64 && c.head_dim != 128) return CF_EUNSUPPORTED;
@@ -58,16 +63,17 @@ inline int check_cache(const cf_cache_config &c, const cf_cache *p, int32_t batc
 }
 // Whether [x, x + bytes) shares memory with a cache of `batch` rows; whether the cache's own buffers do with each other.
 inline size_t cached_rows(const cf_cache_config &c, int32_t batch) { return (size_t)batch * c.n_kv_heads * c.max_seq; }
-inline size_t buffer_bytes(const cf_cache_config &c, int32_t batch) { return cached_rows(c, batch) * c.head_dim * (c.format == CF_CACHE_F16 ? 2 : 1); }
+inline int row_bytes(const cf_cache_config &c) { return c.format == CF_CACHE_F16 ? 2 * c.head_dim : c.format == CF_CACHE_MXFP4 ? c.head_dim / 2 : c.head_dim; }
+inline int row_scale_bytes(const cf_cache_config &c) { return c.format == CF_CACHE_F16 ? 0 : c.format == CF_CACHE_MXFP4 ? c.head_dim / kBlock : 4; }
 inline bool in_cache(const cf_cache_config &c, const cf_cache &p, int32_t batch, const void *x, size_t bytes)
 {
-    const size_t rows = buffer_bytes(c, batch), scales = 4 * cached_rows(c, batch);
+    const size_t rows = cached_rows(c, batch) * row_bytes(c), scales = cached_rows(c, batch) * row_scale_bytes(c);
     if (overlap(x, bytes, p.k, rows) || overlap(x, bytes, p.v, rows)) return true;
     return c.format != CF_CACHE_F16 && (overlap(x, bytes, p.k_scale, scales) || overlap(x, bytes, p.v_scale, scales));
 }
 inline bool tangled(const cf_cache_config &c, const cf_cache &p, int32_t batch)
 {
-    const size_t rows = buffer_bytes(c, batch), scales = 4 * cached_rows(c, batch);
+    const size_t rows = cached_rows(c, batch) * row_bytes(c), scales = cached_rows(c, batch) * row_scale_bytes(c);
     if (overlap(p.k, rows, p.v, rows)) return true;
     return c.format != CF_CACHE_F16 && (overlap(p.k_scale, scales, p.v_scale, scales) || overlap(p.k_scale, scales, p.k, rows) ||
                                         overlap(p.k_scale, scales, p.v, rows) || overlap(p.v_scale, scales, p.k, rows) || overlap(p.v_scale, scales, p.v, rows));
@@ -147,6 +153,38 @@ __device__ __forceinline__ void decode4(uint32_t c, float (&f)[4])
         const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
         f[0] = lo[0], f[1] = lo[1], f[2] = hi[0], f[3] = hi[1];
     }
+}
+
+// ---- 4-bit rows ------------------------------------------------------------------------------------------------------------
+
+// The scale byte of a block from its largest magnitude (top_bits): e + 127 with 2^e the smallest power of two that has top <= 6 * 2^e =
+// 1.5 * 2^(e + 2), held in 2^-23 .. 2^13; 255 for a block that holds an infinity or a NaN.
+__device__ __forceinline__ uint32_t block_scale(uint32_t top)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)top));
+    const int byte = (int)((bits + 0x3fffffu) >> 23) - 2;               // (one more where 1.5 is exceeded)
+    return top < 0x7c00u ? (uint32_t)min(max(byte, 127 - 23), 127 + 13) : 255u;
+}
+__device__ __forceinline__ float scale_of_byte(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+// Eight codes, the first in the lowest half byte: the conversion rounds x / scale to the nearest code, ties to even, and ends at 6.
+__device__ __forceinline__ uint32_t block_codes(h8 v, uint32_t byte)
+{
+    const float scale = scale_of_byte(byte);
+    uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(0u, h2{v[0], v[1]}, scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, h2{v[2], v[3]}, scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, h2{v[4], v[5]}, scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, h2{v[6], v[7]}, scale, 3);
+    return byte == 255u ? 0u : c;
+}
+// Eight codes as fp16, exactly; NaN under a scale of 255 (all exponent bits set).
+__device__ __forceinline__ u32x4 block_values(uint32_t codes, float scale)
+{
+    u32x4 o;
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1));
+    o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2));
+    o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3));
+    return o;
 }
 
 }  // namespace cache

@@ -29,8 +29,10 @@ namespace {
 using namespace cf::cache;
 using cf::tree::f32x4;
 using cf::tree::Keys;
+using cf::tree::Keys4;
 using cf::tree::mfma16;
 using cf::tree::Values;
+using cf::tree::Values4;
 
 constexpr int kMaxTokens = 256, kMaskWords = kMaxTokens / 64;
 constexpr int NT = 256, NW = NT / 64;
@@ -100,6 +102,10 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// whether a cached row has one scale that scores and weights are multiplied with (8 bits)
+template <int FMT>
+constexpr bool kRowScale = FMT == CF_CACHE_E4M3 || FMT == CF_CACHE_INT8;
+
 constexpr int kFar = 0x3fffffff;
 
 // In the kernels below no branch inside the loops over the keys depends on the lane: conditions of lanes are selections, and addresses of
@@ -165,7 +171,7 @@ __device__ __forceinline__ void arguments(const TreeArgs &a, const Sequence &sq,
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int i = 16 * (e >> 2) + 4 * g + (e & 3), j = j0 + i;
-        x[e] = s[e >> 2][e & 3] * (FMT != CF_CACHE_F16 ? kscale[e >> 2][e & 3] : to_score);
+        x[e] = s[e >> 2][e & 3] * (kRowScale<FMT> ? kscale[e >> 2][e & 3] : to_score);
         bool seen = bits >> i & 1;
         if constexpr (FORMS) {
             int key_at = j;
@@ -207,7 +213,7 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
                                       float to_score, const f32x4 (&s)[NR][2], const f32x4 (&kscale)[2], const f32x4 (&vscale)[2], Sums<HD> (&sum)[NR],
                                       h8 (&w)[NR])
 {
-    constexpr bool SCALED = FMT != CF_CACHE_F16;
+    constexpr bool SCALED = kRowScale<FMT>;
     float add[NR], most[NR];
     for (int pass = 0;; ++pass) {
         float highest = 0.f;
@@ -278,14 +284,22 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
 // rows, up to 0.3.)
 //
 // The sums of those among P pieces of W adjacent values, from dimension d0 + 16 p on, of the 32 keys from j0 on, for one row of queries.
+// (vr: the rows, in 4 bits their scales.)
 template <int HD, int FMT, bool FORMS, int P, int W>
 __device__ __forceinline__ void add_unfit(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row &row, __amdgpu_buffer_rsrc_t vr, int j0, int c, int g,
                                           int d0, float (&special)[P][W])
 {
-    constexpr int VB = kValueBytes<FMT>, ROW = HD * VB, DW = W * VB / 4;
-    Values<HD, FMT> vals;                                           // is there one at all
-    vals.load(vr, Values<HD, FMT>::offset(c, g) + (uint32_t)j0 * ROW);
-    if (!__any(vals.take_out_unfit())) return;
+    constexpr int VB = kValueBytes<FMT>, ROW = HD * VB, DW = W * VB / 4, SROW = HD / kBlock;
+    uint32_t some = 0;                                              // is there one at all
+    if constexpr (FMT == CF_CACHE_MXFP4) {
+#pragma unroll
+        for (int i = 0; i < SROW / 2; ++i) some |= __builtin_amdgcn_raw_buffer_load_b8(vr, (uint32_t)j0 * SROW + 64 * i + 16 * g + c, 0, 0) == 255;
+    } else {
+        Values<HD, FMT> vals;
+        vals.load(vr, Values<HD, FMT>::offset(c, g) + (uint32_t)j0 * ROW);
+        some = vals.take_out_unfit();
+    }
+    if (!__any(some)) return;
     const uint32_t bits = seen_bits(sq.tree != nullptr, a.words, row.mask, row.tok, j0, sq.len, sq.n);
 #pragma unroll 1
     for (int i = 0; i < 32; ++i) {
@@ -293,6 +307,15 @@ __device__ __forceinline__ void add_unfit(const TreeArgs &a, const Sequence &sq,
         if (FORMS && a.window > 0) {
             const int key_at = j0 + i < sq.len ? j0 + i : new_at[min(j0 + i - sq.len, sq.n - 1)];
             seen = seen && row.at - key_at < a.window;
+        }
+        if constexpr (FMT == CF_CACHE_MXFP4) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const bool bad = __builtin_amdgcn_raw_buffer_load_b8(vr, (uint32_t)(j0 + i) * SROW + (d0 + 16 * p) / kBlock, 0, 0) == 255;
+#pragma unroll
+                for (int e = 0; e < W; ++e) special[p][e] += seen && bad ? __builtin_nanf("") : 0.f;
+            }
+            continue;
         }
         uint32_t x[P][DW];
 #pragma unroll
@@ -561,6 +584,103 @@ __device__ __forceinline__ int join_lanes(int splits, int rows, int slots)
     return lanes;
 }
 
+// What the wavefronts of tree_tiles and tree_fours share at their end, and the Lookup before it.
+template <int HD, int NR>
+struct TilesSpace {
+    alignas(16) float smem[NW * 16 * (HD + 4)];
+    float2 ml[NW][16 * NR];
+    Lookup<16 * NR> look_up;
+    int left_out[NW];
+    int before;
+};
+// Their sums joined, and the results stored or handed to the join of the parts.  vr: as for add_unfit.
+template <int HD, int FMT, int NR, bool FORMS>
+__device__ __forceinline__ void finish_tiles(const TreeArgs &a, const Sequence &sq, const Place &place, const Part<FORMS, kStep> &part, int first_row, int live,
+                                             __amdgpu_buffer_rsrc_t vr, bool unfit, Sums<HD> (&sum)[NR], TilesSpace<HD, NR> &space)
+{
+    constexpr int NJ = HD / 16;
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
+    float *smem = space.smem;
+    auto &ml = space.ml;
+    auto &look_up = space.look_up;
+    auto &left_out = space.left_out;
+    // 16 rows at a time
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        sum[r].l = cf::lanes::sum_groups<16>(sum[r].l);
+        if (g == 0) ml[wv][16 * r + c] = make_float2(sum[r].mm, sum[r].l);
+    }
+    if (FMT != CF_CACHE_INT8 && lane == 0) left_out[wv] = unfit;
+    float odd = 0.f;                                                // NaN where a result is not finite
+    constexpr int CH = HD / 8;                                      // a thread has eight dimensions of a row
+    const int row16 = tid / CH, d0 = 8 * (tid % CH);
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        __syncthreads();
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr)
+#pragma unroll
+            for (int j = 0; j < NJ; j += 4)
+                *reinterpret_cast<float4 *>(smem + (wv * 16 + c) * (HD + 4) + NJ * (4 * g + rr) + j) =
+                    make_float4(sum[r].acc[j][rr], sum[r].acc[j + 1][rr], sum[r].acc[j + 2][rr], sum[r].acc[j + 3][rr]);
+        __syncthreads();
+        const int i = 16 * r + row16;
+        if (row16 < 16 && i < live) {
+            float m = kNone, total = 0.f, o[8] = {};
+#pragma unroll
+            for (int k = 0; k < NW; ++k) m = fmaxf(m, ml[k][i].x);
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                const float f = exp2_(ml[k][i].x - m);
+                const float *src = smem + (k * 16 + row16) * (HD + 4) + d0;
+                total += f * ml[k][i].y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] += f * src[e];
+            }
+            if (FMT != CF_CACHE_INT8) odd += ((o[0] + o[1]) + (o[2] + o[3])) * 0.f + ((o[4] + o[5]) + (o[6] + o[7])) * 0.f;
+            if (a.splits > 1) {
+                const Partials to(a, HD);
+                const uint32_t at = (uint32_t)place.unit * a.padded + first_row + i;
+                const f32x4 lo = {o[0], o[1], o[2], o[3]}, hi = {o[4], o[5], o[6], o[7]};
+                if (a.arrived) {
+                    to.put<kThrough>(at, d0, lo), to.put<kThrough>(at, d0 + 4, hi);
+                    if (d0 == 0) to.put_ml<kThrough>(at, m, total);
+                } else {
+                    to.put<0>(at, d0, lo), to.put<0>(at, d0 + 4, hi);
+                    if (d0 == 0) to.put_ml<0>(at, m, total);
+                }
+            } else {
+                const float inv = total == 0.f ? 0.f : kValueUnit<FMT> / total;
+                h8 res;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) res[e] = (_Float16)(o[e] * inv);
+                *reinterpret_cast<h8 *>(out_row(a, place, first_row + i, HD) + d0) = res;
+            }
+        }
+    }
+    if constexpr (FMT != CF_CACHE_INT8) {
+        const bool all = __any(odd != 0.f);
+        if (all || __builtin_amdgcn_readfirstlane(left_out[0] | left_out[1] | left_out[2] | left_out[3])) {
+#pragma unroll 1
+            for (int r = 0; r < NR; ++r) {
+                const int i = min(16 * r + row16, live - 1);
+                const int tok = (first_row + i) / a.group;
+                const Row mine = {tok, look_up.mask[i], FORMS ? sq.position(tok) : 0, 0.f};
+                float special[1][8] = {}, total = 0.f;
+                for (int k = 0; k < NW; ++k) total += ml[k][i].y;
+                for (int s = part.begin; s < part.end; ++s)
+                    if (all || (s + 1) * kStep > sq.len || s * kStep < part.all_from)
+                        add_unfit<HD, FMT, FORMS, 1, 8>(a, sq, look_up.at, mine, vr, s * kStep, c, g, d0, special);
+                if (row16 < 16 && 16 * r + row16 < live) put_special<HD, 8>(a, place, first_row + i, d0, total, special[0]);
+            }
+        }
+    }
+    if (a.splits > 1 && a.arrived) {
+        if (last_to_arrive(a, place, space.before))
+            join_rows<HD, NT, kThrough>(a, place, first_row, live, join_lanes(a.splits, live, NT / CH), kValueUnit<FMT>, *reinterpret_cast<JoinSpace<HD, NT> *>(smem));
+    }
+}
+
 // Few rows: reading the keys and values is the work.  Every wavefront has its own steps, so that no barrier holds up its loads: the next step's
 // keys are requested as soon as this one's are used, and its values.  The four wavefronts' sums are joined once, through LDS.
 // Bound: memory where the cache is long (one token over 32768 e4m3 rows, 64 heads: 69 MB in 14.0 us, 4.9 TB/s, then the join; a copy
@@ -572,12 +692,10 @@ template <int HD, int FMT, int NR, bool FORMS>
 __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
 {
     constexpr int KS = HD / 32, NJ = HD / 16, ROW = HD * kValueBytes<FMT>;
-    constexpr bool SCALED = FMT != CF_CACHE_F16;
-    __shared__ float smem[NW * 16 * (HD + 4)];
-    __shared__ float2 ml[NW][16 * NR];
-    __shared__ Lookup<16 * NR> look_up;
+    constexpr bool SCALED = kRowScale<FMT>;
+    __shared__ TilesSpace<HD, NR> space;
     __shared__ alignas(16) float scales[NW][2][kStep];
-    __shared__ int left_out[NW];
+    Lookup<16 * NR> &look_up = space.look_up;
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
     const Place place(a);
     if (place.unit >= a.units) return;
@@ -668,82 +786,92 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
         step = next;
     }
 
-    // ---- the wavefronts' results joined, 16 rows at a time
+    finish_tiles<HD, FMT, NR, FORMS>(a, sq, place, part, first_row, live, vr, unfit, sum, space);
+}
+
+// The same over a cache held in 4 bits.  A step is 4 KB of codes, half of what 8 bits have, so that a wavefront keeps DEPTH steps of loads in
+// flight (all unconditional: a step behind the last one is one of keys that nobody sees).
+template <int HD, int NR, bool FORMS, int DEPTH>
+__global__ __launch_bounds__(NT, 2) void tree_fours(const TreeArgs a)
+{
+    constexpr int FMT = CF_CACHE_MXFP4, KS = HD / 32, NJ = HD / 16, ROW = HD / 2, SROW = HD / kBlock;
+    __shared__ TilesSpace<HD, NR> space;
+    Lookup<16 * NR> &look_up = space.look_up;
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const Place place(a);
+    if (place.unit >= a.units) return;
+    const Sequence sq(a, place.b);
+    const int first_row = place.block * (16 * NR), live = min(sq.n * a.group - first_row, 16 * NR);
+    if (live <= 0) return;
+
+    h8 q[NR][KS];
+    Row row[NR];
+    int nearest = kFar, farthest = -kFar;                           // of the positions of the block's tokens
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        sum[r].l = cf::lanes::sum_groups<16>(sum[r].l);
-        if (g == 0) ml[wv][16 * r + c] = make_float2(sum[r].mm, sum[r].l);
+    for (int r = 0; r < NR; ++r)
+        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + 16 * r + c, look_up.mask[16 * r + c], q[r], nearest, farthest, [&](int ks) { return Keys4<HD>::dim(ks, g); });
+    if (FORMS && a.window > 0)
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
+    const Part<FORMS, kStep> part(a, sq, place, nearest, farthest);
+
+    const size_t slice = (size_t)place.bh * a.max_seq;
+    const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
+    const __amdgpu_buffer_rsrc_t ksr = cf::buffer_of(reinterpret_cast<const char *>(a.k_scale) + slice * SROW, (uint32_t)sq.end * SROW);
+    const __amdgpu_buffer_rsrc_t vsr = cf::buffer_of(reinterpret_cast<const char *>(a.v_scale) + slice * SROW, (uint32_t)sq.end * SROW);
+    const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
+
+    Keys4<HD> keys[DEPTH];
+    Values4<HD> vals[DEPTH];
+    Sums<HD> sum[NR];
+    bool careful = false, unfit = false;                            // unfit: NaN were left out of the product
+    const f32x4 no_scale[2] = {};
+    if (part.has(wv))
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int j0 = part.at(wv + d * NW) * kStep;
+            keys[d].load(kr, ksr, j0, c, g);
+            vals[d].load(vr, vsr, j0, c, g);
+        }
+    if (part.end * kStep > sq.len) {
+        fill<FORMS, NT>(a, sq, first_row, live, look_up);
+        lds_barrier();
     }
-    if (FMT != CF_CACHE_INT8 && lane == 0) left_out[wv] = unfit;
-    float odd = 0.f;                                                // NaN where a result is not finite
-    constexpr int CH = HD / 8;                                      // a thread has eight dimensions of a row
-    const int row16 = tid / CH, d0 = 8 * (tid % CH);
+    for (int i = wv; part.has(i); i += DEPTH * NW)
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        __syncthreads();
+        for (int d = 0; d < DEPTH; ++d) {
+            const int j0 = part.has(i + d * NW) ? part.at(i + d * NW) * kStep : sq.end;
+            const bool masked = j0 + kStep > sq.len || j0 < part.all_from;      // (the same for the whole wavefront)
+            const int next = part.at(i + (d + DEPTH) * NW) * kStep;
+            // ---- scores
+            f32x4 s[NR][2];
 #pragma unroll
-        for (int rr = 0; rr < 4; ++rr)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int j = 0; j < NJ; j += 4)
-                *reinterpret_cast<float4 *>(smem + (wv * 16 + c) * (HD + 4) + NJ * (4 * g + rr) + j) =
-                    make_float4(sum[r].acc[j][rr], sum[r].acc[j + 1][rr], sum[r].acc[j + 2][rr], sum[r].acc[j + 3][rr]);
-        __syncthreads();
-        const int i = 16 * r + row16;
-        if (row16 < 16 && i < live) {
-            float m = kNone, total = 0.f, o[8] = {};
+                for (int ks = 0; ks < KS; ++ks) {
+                    const h8 k = keys[d].operand(t, ks);
 #pragma unroll
-            for (int k = 0; k < NW; ++k) m = fmaxf(m, ml[k][i].x);
-#pragma unroll
-            for (int k = 0; k < NW; ++k) {
-                const float f = exp2_(ml[k][i].x - m);
-                const float *src = smem + (k * 16 + row16) * (HD + 4) + d0;
-                total += f * ml[k][i].y;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] += f * src[e];
-            }
-            if (FMT != CF_CACHE_INT8) odd += ((o[0] + o[1]) + (o[2] + o[3])) * 0.f + ((o[4] + o[5]) + (o[6] + o[7])) * 0.f;
-            if (a.splits > 1) {
-                const Partials to(a, HD);
-                const uint32_t at = (uint32_t)place.unit * a.padded + first_row + i;
-                const f32x4 lo = {o[0], o[1], o[2], o[3]}, hi = {o[4], o[5], o[6], o[7]};
-                if (a.arrived) {
-                    to.put<kThrough>(at, d0, lo), to.put<kThrough>(at, d0 + 4, hi);
-                    if (d0 == 0) to.put_ml<kThrough>(at, m, total);
-                } else {
-                    to.put<0>(at, d0, lo), to.put<0>(at, d0 + 4, hi);
-                    if (d0 == 0) to.put_ml<0>(at, m, total);
+                    for (int r = 0; r < NR; ++r) s[r][t] = mfma16(k, q[r][ks], ks ? s[r][t] : f32x4{0.f, 0.f, 0.f, 0.f});
                 }
-            } else {
-                const float inv = total == 0.f ? 0.f : kValueUnit<FMT> / total;
-                h8 res;
+            keys[d].load(kr, ksr, next, c, g);
+            h8 w[NR];
+            weigh<HD, FMT, FORMS, NR>(a, sq, look_up.at, row, g, j0, masked, careful, to_score, s, no_scale, no_scale, sum, w);
+            // ---- values
+            if (masked) unfit = __any(vals[d].take_out_unfit()) || unfit;
+            const auto product = [&](auto pair) {
+                constexpr int PAIR = decltype(pair)::value;
+                h8 v[2];
+                vals[d].template operands<PAIR>(v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) res[e] = (_Float16)(o[e] * inv);
-                *reinterpret_cast<h8 *>(out_row(a, place, first_row + i, HD) + d0) = res;
-            }
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) sum[r].acc[2 * PAIR + j] = mfma16(v[j], w[r], sum[r].acc[2 * PAIR + j]);
+            };
+            product(std::integral_constant<int, 0>()), product(std::integral_constant<int, 1>());
+            if constexpr (NJ == 8) product(std::integral_constant<int, 2>()), product(std::integral_constant<int, 3>());
+            vals[d].load(vr, vsr, next, c, g);
         }
-    }
-    if constexpr (FMT != CF_CACHE_INT8) {
-        const bool all = __any(odd != 0.f);
-        if (all || __builtin_amdgcn_readfirstlane(left_out[0] | left_out[1] | left_out[2] | left_out[3])) {
-#pragma unroll 1
-            for (int r = 0; r < NR; ++r) {
-                const int i = min(16 * r + row16, live - 1);
-                const int tok = (first_row + i) / a.group;
-                const Row mine = {tok, look_up.mask[i], FORMS ? sq.position(tok) : 0, 0.f};
-                float special[1][8] = {}, total = 0.f;
-                for (int k = 0; k < NW; ++k) total += ml[k][i].y;
-                for (int s = part.begin; s < part.end; ++s)
-                    if (all || (s + 1) * kStep > sq.len || s * kStep < part.all_from)
-                        add_unfit<HD, FMT, FORMS, 1, 8>(a, sq, look_up.at, mine, vr, s * kStep, c, g, d0, special);
-                if (row16 < 16 && 16 * r + row16 < live) put_special<HD, 8>(a, place, first_row + i, d0, total, special[0]);
-            }
-        }
-    }
-    if (a.splits > 1 && a.arrived) {
-        __shared__ int before;
-        if (last_to_arrive(a, place, before))
-            join_rows<HD, NT, kThrough>(a, place, first_row, live, join_lanes(a.splits, live, NT / CH), kValueUnit<FMT>, *reinterpret_cast<JoinSpace<HD, NT> *>(smem));
-    }
+    finish_tiles<HD, FMT, NR, FORMS>(a, sq, place, part, first_row, live, vsr, unfit, sum, space);
 }
 
 // Staged steps: 64 rows of keys and of values as fp16 in LDS, two steps deep.  A row of keys is 16 bytes longer than its values, so that the
@@ -785,11 +913,12 @@ __device__ __forceinline__ h8 transposed(const char *v, int first, int dim, int 
 template <int HD, int FMT, int RW, int KG, int NR, bool FORMS>
 __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 {
-    constexpr int WV = RW * KG, KS = HD / 32, NJ = HD / 16, ROW = HD * kValueBytes<FMT>, T = 64 * WV;
-    constexpr bool SCALED = FMT != CF_CACHE_F16;
-    // 16-byte pieces of a row; of the keys of a step, to a thread.  Where there are more threads than pieces the first ones have the keys,
-    // the last ones the values.
-    constexpr int PPR = ROW / 16, ALL = kBlockStep * PPR, PIECES = ALL < T ? 1 : ALL / T, APART = ALL < T ? T - ALL : 0;
+    constexpr bool FOUR = FMT == CF_CACHE_MXFP4;
+    constexpr int WV = RW * KG, KS = HD / 32, NJ = HD / 16, ROW = bytes_of<FMT>(HD), SROW = HD / kBlock, T = 64 * WV;
+    constexpr bool SCALED = kRowScale<FMT>;
+    // 16-byte pieces of a row (in 4 bits quarters of it); of the keys of a step, to a thread.  Where there are more threads than pieces the first
+    // ones have the keys, the last ones the values.
+    constexpr int PB = FOUR ? ROW / 4 : 16, PPR = ROW / PB, ALL = kBlockStep * PPR, PIECES = ALL < T ? 1 : ALL / T, APART = ALL < T ? T - ALL : 0;
     static_assert(ALL % T == 0 || 2 * ALL == T, "every thread stages as much");
     using S = Stage<HD>;
     __shared__ S lds;
@@ -824,6 +953,12 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     const size_t slice = (size_t)place.bh * a.max_seq;
     const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
     const float *scale_src = SCALED ? (wv == 1 ? a.v_scale : a.k_scale) + slice : nullptr;
+    // in 4 bits: of the first threads the keys, of the others the values, and their scales
+    static_assert(!FOUR || (PIECES == 1 && APART == ALL), "one piece to a thread");
+    const bool has_values = 64 * wv >= ALL;
+    const char *scale_bytes = reinterpret_cast<const char *>(has_values ? a.v_scale : a.k_scale) + slice * SROW;
+    const __amdgpu_buffer_rsrc_t four = cf::buffer_of((has_values ? a.v : a.k) + slice * ROW, (uint32_t)sq.end * ROW);
+    const __amdgpu_buffer_rsrc_t four_scale = cf::buffer_of(scale_bytes, FOUR ? (uint32_t)sq.end * SROW : 0u);
     const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
 
     Sums<HD> sum[NR];
@@ -831,8 +966,20 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 
     // ---- staging: requested a step ahead of the one that is written, which is a step ahead of the one that is used
     u32x4 kraw[PIECES], vraw[PIECES];
+    uint32_t power = 0;                                             // scale of a piece in 4 bits
     float scale = 0.f;
     auto request = [&](int step) {
+        if constexpr (FOUR) {
+            const uint32_t at = (uint32_t)step * ALL + tid % ALL;
+            if constexpr (PB == 16) {
+                kraw[0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(four, at * PB, 0, 0));
+            } else {
+                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(four, at * PB, 0, 0));
+                kraw[0] = u32x4{x[0], x[1], 0u, 0u};
+            }
+            power = __builtin_amdgcn_raw_buffer_load_b8(four_scale, at * SROW / PPR, 0, 0);
+            return;
+        }
         const uint32_t off = (uint32_t)step * (kBlockStep * ROW) + 16 * tid;
         if (!APART || 64 * wv < ALL)
 #pragma unroll
@@ -860,6 +1007,18 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
                 *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(2 * col + 1)) = cf::tree::widen<FMT>(raw[2], raw[3]);
             }
         };
+        if constexpr (FOUR) {
+            uint32_t of_piece = power;
+            if (look && has_values) odd = power == 255u, of_piece = power == 255u ? 0u : power;
+            const int piece = tid % ALL;
+            char *dst = has_values ? lds.v[buf] + piece / PPR * S::VROW : lds.k[buf] + piece / PPR * S::KROW;
+            constexpr int CHUNKS = PB / 4;
+#pragma unroll
+            for (int w = 0; w < CHUNKS; ++w)
+                *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(CHUNKS * (piece % PPR) + w)) = block_values(kraw[0][w], cf::cache::scale_of_byte(of_piece));
+            if (look && __any(odd)) left_out = 1;
+            return;
+        }
         if (!APART || 64 * wv < ALL)
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) put(lds.k[buf], S::KROW, kraw[i], tid + T * i, false);
@@ -984,17 +1143,19 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) odd += sum[r].acc[j] * 0.f;
         const bool all = __any((odd[0] + odd[1]) + (odd[2] + odd[3]) != 0.f);
-        if (part.begin < part.end && (all || __builtin_amdgcn_readfirstlane(left_out)))
+        if (part.begin < part.end && (all || __builtin_amdgcn_readfirstlane(left_out))) {
+            const __amdgpu_buffer_rsrc_t value_scales = cf::buffer_of(reinterpret_cast<const char *>(a.v_scale) + slice * SROW, FOUR ? (uint32_t)sq.end * SROW : 0u);
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
                 const int i = my_rows + 16 * r + c;
                 float special[NJ][4] = {};
                 for (int s = 2 * part.begin; s < 2 * part.end; ++s)
-                    if (all || masked_step(s / 2)) add_unfit<HD, FMT, FORMS, NJ, 4>(a, sq, look_up.at, row[r], vr, s * kStep, c, g, 4 * g, special);
+                    if (all || masked_step(s / 2)) add_unfit<HD, FMT, FORMS, NJ, 4>(a, sq, look_up.at, row[r], FOUR ? value_scales : vr, s * kStep, c, g, 4 * g, special);
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
                     if (i < live) put_special<HD, 4>(a, place, first_row + i, 16 * j + 4 * g, sum[r].l, special[j]);
             }
+        }
     }
     if (a.splits > 1 && a.arrived) {
         __shared__ int before;
@@ -1053,9 +1214,19 @@ KernelFn pick_shape(int shape)
         return fn[shape];
     }
 }
+// in 4 bits
+template <int HD, bool FORMS>
+KernelFn pick_four(int shape)
+{
+    if constexpr (FORMS)
+        return shape < 2 ? tree_fours<HD, 1, true, 2> : shape == 2 ? tree_blocks<HD, CF_CACHE_MXFP4, 4, 2, 1, true> : tree_blocks<HD, CF_CACHE_MXFP4, 8, 1, 1, true>;
+    else
+        return shape == 0 ? tree_fours<HD, 1, false, 2> : shape < 4 ? tree_fours<HD, 2, false, 2> : tree_blocks<HD, CF_CACHE_MXFP4, 8, 1, 2, false>;
+}
 template <int HD, bool FORMS>
 KernelFn pick_format(int fmt, int shape)
 {
+    if (fmt == CF_CACHE_MXFP4) return pick_four<HD, FORMS>(shape);
     return fmt == CF_CACHE_F16 ? pick_shape<HD, CF_CACHE_F16, FORMS>(shape) : fmt == CF_CACHE_E4M3 ? pick_shape<HD, CF_CACHE_E4M3, FORMS>(shape) : pick_shape<HD, CF_CACHE_INT8, FORMS>(shape);
 }
 KernelFn pick(int hd, int fmt, int shape, bool forms)
@@ -1251,7 +1422,7 @@ int64_t cf_tree_algorithmic_bytes(const cf_tree_config *cfg, int32_t batch, int3
 {
     if (!cfg) return 0;
     const cf_cache_config &c = cfg->cache;
-    const int64_t row = c.format == CF_CACHE_F16 ? 2 * (int64_t)c.head_dim : (int64_t)c.head_dim + 4;
+    const int64_t row = row_bytes(c) + row_scale_bytes(c);
     const int64_t read = cfg->window > 0 && cfg->window < len ? cfg->window : len;      // cached rows that some token may see
     return (int64_t)batch * (2 * c.n_kv_heads * row * (read + tokens) + 4 * (int64_t)tokens * c.n_q_heads * c.head_dim);
 }

@@ -169,6 +169,81 @@ struct Values {
     }
 };
 
+// ---- 4-bit rows. Both operands are exact fp16 values: the conversions take the block's scale in, one instruction for two values.
+
+// The keys of a step: a quarter of a row (one block of 128 dimensions, half of one of 64) and its scale to a lane.
+template <int HD>
+struct Keys4 {
+    static constexpr int ROW = HD / 2, WORDS = HD / 32, SROW = HD / cache::kBlock;      // bytes of a row; dwords of a quarter; scales of a row
+    uint32_t raw[2][WORDS];
+    uint32_t scale[2];
+    static __device__ __forceinline__ int dim(int ks, int g) { return HD / 4 * g + 8 * ks; }
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t sr, int j0, int c, int g)
+    {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t off = (j0 + 16 * t + c) * ROW + 4 * WORDS * g;
+            if constexpr (WORDS == 4) {
+                const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+#pragma unroll
+                for (int w = 0; w < 4; ++w) raw[t][w] = x[w];
+            } else {
+                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+                raw[t][0] = x[0], raw[t][1] = x[1];
+            }
+            scale[t] = __builtin_amdgcn_raw_buffer_load_b8(sr, (j0 + 16 * t + c) * SROW + g * SROW / 4, 0, 0);
+        }
+    }
+    __device__ __forceinline__ h8 operand(int t, int ks) const
+    {
+        return __builtin_bit_cast(h8, cache::block_values(raw[t][ks], cache::scale_of_byte(scale[t])));
+    }
+};
+
+// The values of a step: NJ adjacent dimensions of eight rows to a lane, converted two dimensions at a time and then transposed.
+template <int HD>
+struct Values4 {
+    static constexpr int NJ = HD / 16, ROW = HD / 2, SROW = HD / cache::kBlock;
+    uint32_t raw[8], scale[8];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t sr, int j0, int c, int g)
+    {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const uint32_t row = j0 + 4 * g + (u < 4 ? u : 12 + u);
+            if constexpr (NJ == 8)
+                raw[u] = __builtin_amdgcn_raw_buffer_load_b32(r, row * ROW + 4 * c, 0, 0);
+            else
+                raw[u] = __builtin_amdgcn_raw_buffer_load_b16(r, row * ROW + 2 * c, 0, 0);
+            scale[u] = __builtin_amdgcn_raw_buffer_load_b8(sr, row * SROW + NJ * c / cache::kBlock, 0, 0);
+        }
+    }
+    // the operands of dimensions NJ c + 2 PAIR and NJ c + 2 PAIR + 1
+    template <int PAIR>
+    __device__ __forceinline__ void operands(h8 (&f)[2]) const
+    {
+        u32x4 o[2];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[2 * w], cache::scale_of_byte(scale[2 * w]), PAIR));
+            const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[2 * w + 1], cache::scale_of_byte(scale[2 * w + 1]), PAIR));
+            o[0][w] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+            o[1][w] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+        }
+        f[0] = __builtin_bit_cast(h8, o[0]), f[1] = __builtin_bit_cast(h8, o[1]);
+    }
+    // Takes NaN blocks out (their values count as zeros); not 0 if there were some.
+    __device__ __forceinline__ uint32_t take_out_unfit()
+    {
+        uint32_t odd = 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            odd |= scale[u] == 255u;
+            scale[u] = scale[u] == 255u ? 0u : scale[u];
+        }
+        return odd;
+    }
+};
+
 }  // namespace tree
 }  // namespace cf
 
