@@ -79,11 +79,6 @@ __device__ __forceinline__ _Float16 scaled(int sum, float sx, float sw)
     return (_Float16)y;
 }
 
-// 16 bytes a lane from memory to `to` + 16 * lane in LDS (`to` is the same in all lanes).
-__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t r, char *to, uint32_t at, uint32_t also)
-{
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 16, at, also, 0, 0);
-}
 // What this wavefront requested is in LDS but for its last LEFT requests, and so it is with all others.
 template <int LEFT>
 __device__ __forceinline__ void landed_barrier()
@@ -130,9 +125,9 @@ __global__ __launch_bounds__(64 * WAVES) void linear_stream(const LinearArgs a)
         const int k0 = 128 * piece_of(i);
         const uint32_t at = row_at + (k0 + 16 * chunk < a.n_in ? (uint32_t)k0 : 0x80000000u);      // (behind the end, and rows that are not there: no access)
 #pragma unroll
-        for (int r = 0; r < COLS / 8; ++r) to_lds(wr, ring + d * PLACE + 1024 * r, at + (uint32_t)(8 * r) * a.n_in, 0);
+        for (int r = 0; r < COLS / 8; ++r) cf::to_lds(wr, ring + d * PLACE + 1024 * r, at + (uint32_t)(8 * r) * a.n_in, 0);
 #pragma unroll
-        for (int r = 0; r < ROWS / 8; ++r) to_lds(xr, ring + d * PLACE + COLS * 128 + 1024 * r, at + (uint32_t)(8 * r) * a.n_in, 0);
+        for (int r = 0; r < ROWS / 8; ++r) cf::to_lds(xr, ring + d * PLACE + COLS * 128 + 1024 * r, at + (uint32_t)(8 * r) * a.n_in, 0);
     };
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) request(d, d);
@@ -222,9 +217,9 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tiles(const LinearArgs a)
         const int k0 = turned(i) * kTileStep;
         const int back = max(k0 + 16 * chunk - (a.n_in - 16), 0);   // chunks behind the end: any other one
 #pragma unroll
-        for (int i = 0; i < XL; ++i) to_lds(xr, to + 1024 * (wv + WAVES * i), x_at[i] - back, k0);
+        for (int i = 0; i < XL; ++i) cf::to_lds(xr, to + 1024 * (wv + WAVES * i), x_at[i] - back, k0);
 #pragma unroll
-        for (int i = 0; i < WL; ++i) to_lds(wr, to + BM * kTileStep + 1024 * (wv + WAVES * i), w_at[i] - back, k0);
+        for (int i = 0; i < WL; ++i) cf::to_lds(wr, to + BM * kTileStep + 1024 * (wv + WAVES * i), w_at[i] - back, k0);
     };
     i32x16 sum[TM][TN] = {};
 #pragma unroll

@@ -32,6 +32,14 @@ struct Part {
     __device__ __forceinline__ h8 ld(uint32_t off) const { return __builtin_bit_cast(h8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, AUX)); }
 };
 
+// 16 bytes a lane from memory to `to` + 16 * lane in LDS (`to` is the same in all lanes), without a stay in registers.  Counted by vmcnt like a load;
+// nothing but a wait of the wavefront's own orders it with its reads of LDS.  A lane outside of the buffer makes no access; what its place then holds
+// is not to be used.
+__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t r, char *to, uint32_t at, uint32_t also = 0)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 16, at, also, 0, 0);
+}
+
 // What fdiv takes for a divisor of this workgroup.
 __device__ __forceinline__ float reciprocal(int d) { return __builtin_amdgcn_rcpf((float)d); }
 

@@ -1,10 +1,11 @@
 // Attention of drafted tokens over a key/value cache (cf_tree_* in include/cfdecode.h).
 //
 // The rows of one KV head's queries (token t, query head hh of the group: row t * group + hh) are cut into blocks, the keys of a sequence
-// into parts; a workgroup takes one block over one part.  Scores and weighted values are matrix products (cf_tree_device.h).  Two
+// into parts; a workgroup takes one block over one part.  Scores and weighted values are matrix products (cf_tree_device.h).  Three
 // kernels: with blocks of up to 32 rows the four wavefronts of a workgroup take steps of 32 keys in turn, each with all rows, and keys and
 // values go from memory into registers as the operands want them (tree_tiles); with larger ones the wavefronts divide the rows and share
-// steps of 64 keys, which are staged in LDS as fp16 (tree_blocks), so that 8-bit codes are converted once for all rows.
+// steps of 64 keys, which are staged in LDS as fp16 (tree_blocks), so that 8-bit codes are converted once for all rows.  A 4-bit cache has
+// blocks of up to 32 rows alone, whose values go through LDS that each wavefront has for itself (tree_fours).
 //
 // Softmax in one pass.  Every row keeps a reference mm, the sum l of 2^(x_j - mm) and the sums of w_j v_j with
 // w_j = 2^(x_j - mm) * scale_j (x_j: score in units of log2 e, scale_j: scale of an 8-bit value row, else 1), so that values enter the
@@ -272,6 +273,82 @@ __device__ __forceinline__ void weigh(const TreeArgs &a, const Sequence &sq, con
             careful = careful || __any(moves && fabsf(to) > kCareful);
         }
     }
+#pragma unroll
+    for (int r = 0; r < NR; ++r) sum[r].l += add[r];
+}
+
+// The same for tree_fours, without scales of rows, and with the ordinary way of all rows apart: 16 registers fewer there and, without a branch for
+// every row, 9 % less time at 32 rows a wavefront.  (The other kernels, whose scales are in the way, would need more registers.)
+//
+// Exponentials, which are the weights, as an operand; their sum and the largest one.
+__device__ __forceinline__ void take(const float (&p)[8], h8 &w, float &add, float &most)
+{
+    add = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    most = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) most = fmaxf(fmaxf(most, p[e]), p[e + 1]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = (_Float16)p[e];
+}
+template <int HD, int FMT, bool FORMS, int NR>
+__device__ __forceinline__ void weigh_apart(const TreeArgs &a, const Sequence &sq, const int *new_at, const Row (&row)[NR], int g, int j0, bool masked, bool &careful,
+                                            float to_score, const f32x4 (&s)[NR][2], Sums<HD> (&sum)[NR], h8 (&w)[NR])
+{
+    static_assert(!kRowScale<FMT>, "no scales");
+    const f32x4 none[2] = {};
+    float add[NR], most[NR], highest = 0.f;
+    const bool ordinary = !(FORMS || masked || careful);
+    if (ordinary)
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = exp2_(fmaf(s[r][e >> 2][e & 3], to_score, -sum[r].mm));
+            take(p, w[r], add[r], most[r]);
+            highest = r ? fmaxf(highest, most[r]) : most[r];
+        }
+    if (!ordinary || __any(highest > kMostWeight))
+        for (int pass = ordinary;; ++pass) {
+            if (pass)
+                // some weight is too large: rows with such a one get a new reference
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    float x[8], top = kNone;
+                    bool sees[8];
+                    arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], none, x, sees);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e] == -INFINITY ? kNone : x[e]);
+                    top = cf::lanes::max_groups<16>(top);
+                    const bool moves = cf::lanes::max_groups<16>(most[r]) > kMostWeight;
+                    const float to = moves ? top - kTopExponent : sum[r].mm, by = moves ? exp2_(sum[r].mm - to) : 1.f;
+                    sum[r].mm = to;
+                    sum[r].l *= by;
+#pragma unroll
+                    for (int j = 0; j < HD / 16; ++j) sum[r].acc[j] *= by;
+                    careful = careful || __any(moves && fabsf(to) > kCareful);
+                }
+            highest = 0.f;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                float p[8];
+                bool sees[8];
+                const bool large = fabsf(sum[r].mm) > kCareful;
+                arguments<FMT, FORMS>(a, sq, new_at, row[r], g, j0, masked, to_score, s[r], none, p, sees);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float rounded = p[e] - sum[r].mm;
+                    float y = rounded;
+                    if (!FORMS && !masked) {
+                        const float fused = fmaf(s[r][e >> 2][e & 3], to_score, -sum[r].mm);
+                        y = large ? rounded : fused;
+                    }
+                    p[e] = exp2_(y);
+                }
+                take(p, w[r], add[r], most[r]);
+                highest = fmaxf(highest, most[r]);
+            }
+            if (pass || !__any(highest > kMostWeight)) break;
+        }
 #pragma unroll
     for (int r = 0; r < NR; ++r) sum[r].l += add[r];
 }
@@ -585,9 +662,12 @@ __device__ __forceinline__ int join_lanes(int splits, int rows, int slots)
 }
 
 // What the wavefronts of tree_tiles and tree_fours share at their end, and the Lookup before it.
+template <int HD>
+struct alignas(16) TilesSums {
+    float of[NW * 16 * (HD + 4)];
+};
 template <int HD, int NR>
 struct TilesSpace {
-    alignas(16) float smem[NW * 16 * (HD + 4)];
     float2 ml[NW][16 * NR];
     Lookup<16 * NR> look_up;
     int left_out[NW];
@@ -596,11 +676,11 @@ struct TilesSpace {
 // Their sums joined, and the results stored or handed to the join of the parts.  vr: as for add_unfit.
 template <int HD, int FMT, int NR, bool FORMS>
 __device__ __forceinline__ void finish_tiles(const TreeArgs &a, const Sequence &sq, const Place &place, const Part<FORMS, kStep> &part, int first_row, int live,
-                                             __amdgpu_buffer_rsrc_t vr, bool unfit, Sums<HD> (&sum)[NR], TilesSpace<HD, NR> &space)
+                                             __amdgpu_buffer_rsrc_t vr, bool unfit, Sums<HD> (&sum)[NR], TilesSums<HD> &sums, TilesSpace<HD, NR> &space)
 {
     constexpr int NJ = HD / 16;
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
-    float *smem = space.smem;
+    float *smem = sums.of;
     auto &ml = space.ml;
     auto &look_up = space.look_up;
     auto &left_out = space.left_out;
@@ -621,8 +701,11 @@ __device__ __forceinline__ void finish_tiles(const TreeArgs &a, const Sequence &
         for (int rr = 0; rr < 4; ++rr)
 #pragma unroll
             for (int j = 0; j < NJ; j += 4)
-                *reinterpret_cast<float4 *>(smem + (wv * 16 + c) * (HD + 4) + NJ * (4 * g + rr) + j) =
-                    make_float4(sum[r].acc[j][rr], sum[r].acc[j + 1][rr], sum[r].acc[j + 2][rr], sum[r].acc[j + 3][rr]);
+                if constexpr (FMT == CF_CACHE_MXFP4)                // (its sums are those of dimensions 16 j + 4 g .. 16 j + 4 g + 3)
+                    *reinterpret_cast<f32x4 *>(smem + (wv * 16 + c) * (HD + 4) + 4 * NJ * rr + 4 * j + 4 * g) = sum[r].acc[(NJ * rr + j) / 4];
+                else
+                    *reinterpret_cast<float4 *>(smem + (wv * 16 + c) * (HD + 4) + NJ * (4 * g + rr) + j) =
+                        make_float4(sum[r].acc[j][rr], sum[r].acc[j + 1][rr], sum[r].acc[j + 2][rr], sum[r].acc[j + 3][rr]);
         __syncthreads();
         const int i = 16 * r + row16;
         if (row16 < 16 && i < live) {
@@ -693,6 +776,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
 {
     constexpr int KS = HD / 32, NJ = HD / 16, ROW = HD * kValueBytes<FMT>;
     constexpr bool SCALED = kRowScale<FMT>;
+    __shared__ TilesSums<HD> sums;
     __shared__ TilesSpace<HD, NR> space;
     __shared__ alignas(16) float scales[NW][2][kStep];
     Lookup<16 * NR> &look_up = space.look_up;
@@ -786,92 +870,7 @@ __global__ __launch_bounds__(NT, 2) void tree_tiles(const TreeArgs a)
         step = next;
     }
 
-    finish_tiles<HD, FMT, NR, FORMS>(a, sq, place, part, first_row, live, vr, unfit, sum, space);
-}
-
-// The same over a cache held in 4 bits.  A step is 4 KB of codes, half of what 8 bits have, so that a wavefront keeps DEPTH steps of loads in
-// flight (all unconditional: a step behind the last one is one of keys that nobody sees).
-template <int HD, int NR, bool FORMS, int DEPTH>
-__global__ __launch_bounds__(NT, 2) void tree_fours(const TreeArgs a)
-{
-    constexpr int FMT = CF_CACHE_MXFP4, KS = HD / 32, NJ = HD / 16, ROW = HD / 2, SROW = HD / kBlock;
-    __shared__ TilesSpace<HD, NR> space;
-    Lookup<16 * NR> &look_up = space.look_up;
-    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
-    const Place place(a);
-    if (place.unit >= a.units) return;
-    const Sequence sq(a, place.b);
-    const int first_row = place.block * (16 * NR), live = min(sq.n * a.group - first_row, 16 * NR);
-    if (live <= 0) return;
-
-    h8 q[NR][KS];
-    Row row[NR];
-    int nearest = kFar, farthest = -kFar;                           // of the positions of the block's tokens
-#pragma unroll
-    for (int r = 0; r < NR; ++r)
-        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + 16 * r + c, look_up.mask[16 * r + c], q[r], nearest, farthest, [&](int ks) { return Keys4<HD>::dim(ks, g); });
-    if (FORMS && a.window > 0)
-#pragma unroll
-        for (int s = 1; s < 16; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
-    const Part<FORMS, kStep> part(a, sq, place, nearest, farthest);
-
-    const size_t slice = (size_t)place.bh * a.max_seq;
-    const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
-    const __amdgpu_buffer_rsrc_t ksr = cf::buffer_of(reinterpret_cast<const char *>(a.k_scale) + slice * SROW, (uint32_t)sq.end * SROW);
-    const __amdgpu_buffer_rsrc_t vsr = cf::buffer_of(reinterpret_cast<const char *>(a.v_scale) + slice * SROW, (uint32_t)sq.end * SROW);
-    const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
-
-    Keys4<HD> keys[DEPTH];
-    Values4<HD> vals[DEPTH];
-    Sums<HD> sum[NR];
-    bool careful = false, unfit = false;                            // unfit: NaN were left out of the product
-    const f32x4 no_scale[2] = {};
-    if (part.has(wv))
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int j0 = part.at(wv + d * NW) * kStep;
-            keys[d].load(kr, ksr, j0, c, g);
-            vals[d].load(vr, vsr, j0, c, g);
-        }
-    if (part.end * kStep > sq.len) {
-        fill<FORMS, NT>(a, sq, first_row, live, look_up);
-        lds_barrier();
-    }
-    for (int i = wv; part.has(i); i += DEPTH * NW)
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int j0 = part.has(i + d * NW) ? part.at(i + d * NW) * kStep : sq.end;
-            const bool masked = j0 + kStep > sq.len || j0 < part.all_from;      // (the same for the whole wavefront)
-            const int next = part.at(i + (d + DEPTH) * NW) * kStep;
-            // ---- scores
-            f32x4 s[NR][2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const h8 k = keys[d].operand(t, ks);
-#pragma unroll
-                    for (int r = 0; r < NR; ++r) s[r][t] = mfma16(k, q[r][ks], ks ? s[r][t] : f32x4{0.f, 0.f, 0.f, 0.f});
-                }
-            keys[d].load(kr, ksr, next, c, g);
-            h8 w[NR];
-            weigh<HD, FMT, FORMS, NR>(a, sq, look_up.at, row, g, j0, masked, careful, to_score, s, no_scale, no_scale, sum, w);
-            // ---- values
-            if (masked) unfit = __any(vals[d].take_out_unfit()) || unfit;
-            const auto product = [&](auto pair) {
-                constexpr int PAIR = decltype(pair)::value;
-                h8 v[2];
-                vals[d].template operands<PAIR>(v);
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int r = 0; r < NR; ++r) sum[r].acc[2 * PAIR + j] = mfma16(v[j], w[r], sum[r].acc[2 * PAIR + j]);
-            };
-            product(std::integral_constant<int, 0>()), product(std::integral_constant<int, 1>());
-            if constexpr (NJ == 8) product(std::integral_constant<int, 2>()), product(std::integral_constant<int, 3>());
-            vals[d].load(vr, vsr, next, c, g);
-        }
-    finish_tiles<HD, FMT, NR, FORMS>(a, sq, place, part, first_row, live, vsr, unfit, sum, space);
+    finish_tiles<HD, FMT, NR, FORMS>(a, sq, place, part, first_row, live, vr, unfit, sum, sums, space);
 }
 
 // Staged steps: 64 rows of keys and of values as fp16 in LDS, two steps deep.  A row of keys is 16 bytes longer than its values, so that the
@@ -913,12 +912,11 @@ __device__ __forceinline__ h8 transposed(const char *v, int first, int dim, int 
 template <int HD, int FMT, int RW, int KG, int NR, bool FORMS>
 __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 {
-    constexpr bool FOUR = FMT == CF_CACHE_MXFP4;
-    constexpr int WV = RW * KG, KS = HD / 32, NJ = HD / 16, ROW = bytes_of<FMT>(HD), SROW = HD / kBlock, T = 64 * WV;
+    constexpr int WV = RW * KG, KS = HD / 32, NJ = HD / 16, ROW = HD * kValueBytes<FMT>, T = 64 * WV;
     constexpr bool SCALED = kRowScale<FMT>;
-    // 16-byte pieces of a row (in 4 bits quarters of it); of the keys of a step, to a thread.  Where there are more threads than pieces the first
-    // ones have the keys, the last ones the values.
-    constexpr int PB = FOUR ? ROW / 4 : 16, PPR = ROW / PB, ALL = kBlockStep * PPR, PIECES = ALL < T ? 1 : ALL / T, APART = ALL < T ? T - ALL : 0;
+    // 16-byte pieces of a row; of the keys of a step, to a thread.  Where there are more threads than pieces the first ones have the keys,
+    // the last ones the values.
+    constexpr int PPR = ROW / 16, ALL = kBlockStep * PPR, PIECES = ALL < T ? 1 : ALL / T, APART = ALL < T ? T - ALL : 0;
     static_assert(ALL % T == 0 || 2 * ALL == T, "every thread stages as much");
     using S = Stage<HD>;
     __shared__ S lds;
@@ -953,12 +951,6 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
     const size_t slice = (size_t)place.bh * a.max_seq;
     const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
     const float *scale_src = SCALED ? (wv == 1 ? a.v_scale : a.k_scale) + slice : nullptr;
-    // in 4 bits: of the first threads the keys, of the others the values, and their scales
-    static_assert(!FOUR || (PIECES == 1 && APART == ALL), "one piece to a thread");
-    const bool has_values = 64 * wv >= ALL;
-    const char *scale_bytes = reinterpret_cast<const char *>(has_values ? a.v_scale : a.k_scale) + slice * SROW;
-    const __amdgpu_buffer_rsrc_t four = cf::buffer_of((has_values ? a.v : a.k) + slice * ROW, (uint32_t)sq.end * ROW);
-    const __amdgpu_buffer_rsrc_t four_scale = cf::buffer_of(scale_bytes, FOUR ? (uint32_t)sq.end * SROW : 0u);
     const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
 
     Sums<HD> sum[NR];
@@ -966,20 +958,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 
     // ---- staging: requested a step ahead of the one that is written, which is a step ahead of the one that is used
     u32x4 kraw[PIECES], vraw[PIECES];
-    uint32_t power = 0;                                             // scale of a piece in 4 bits
     float scale = 0.f;
     auto request = [&](int step) {
-        if constexpr (FOUR) {
-            const uint32_t at = (uint32_t)step * ALL + tid % ALL;
-            if constexpr (PB == 16) {
-                kraw[0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(four, at * PB, 0, 0));
-            } else {
-                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(four, at * PB, 0, 0));
-                kraw[0] = u32x4{x[0], x[1], 0u, 0u};
-            }
-            power = __builtin_amdgcn_raw_buffer_load_b8(four_scale, at * SROW / PPR, 0, 0);
-            return;
-        }
         const uint32_t off = (uint32_t)step * (kBlockStep * ROW) + 16 * tid;
         if (!APART || 64 * wv < ALL)
 #pragma unroll
@@ -1007,18 +987,6 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
                 *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(2 * col + 1)) = cf::tree::widen<FMT>(raw[2], raw[3]);
             }
         };
-        if constexpr (FOUR) {
-            uint32_t of_piece = power;
-            if (look && has_values) odd = power == 255u, of_piece = power == 255u ? 0u : power;
-            const int piece = tid % ALL;
-            char *dst = has_values ? lds.v[buf] + piece / PPR * S::VROW : lds.k[buf] + piece / PPR * S::KROW;
-            constexpr int CHUNKS = PB / 4;
-#pragma unroll
-            for (int w = 0; w < CHUNKS; ++w)
-                *reinterpret_cast<u32x4 *>(dst + 16 * chunk_at(CHUNKS * (piece % PPR) + w)) = block_values(kraw[0][w], cf::cache::scale_of_byte(of_piece));
-            if (look && __any(odd)) left_out = 1;
-            return;
-        }
         if (!APART || 64 * wv < ALL)
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) put(lds.k[buf], S::KROW, kraw[i], tid + T * i, false);
@@ -1143,19 +1111,17 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) odd += sum[r].acc[j] * 0.f;
         const bool all = __any((odd[0] + odd[1]) + (odd[2] + odd[3]) != 0.f);
-        if (part.begin < part.end && (all || __builtin_amdgcn_readfirstlane(left_out))) {
-            const __amdgpu_buffer_rsrc_t value_scales = cf::buffer_of(reinterpret_cast<const char *>(a.v_scale) + slice * SROW, FOUR ? (uint32_t)sq.end * SROW : 0u);
+        if (part.begin < part.end && (all || __builtin_amdgcn_readfirstlane(left_out)))
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
                 const int i = my_rows + 16 * r + c;
                 float special[NJ][4] = {};
                 for (int s = 2 * part.begin; s < 2 * part.end; ++s)
-                    if (all || masked_step(s / 2)) add_unfit<HD, FMT, FORMS, NJ, 4>(a, sq, look_up.at, row[r], FOUR ? value_scales : vr, s * kStep, c, g, 4 * g, special);
+                    if (all || masked_step(s / 2)) add_unfit<HD, FMT, FORMS, NJ, 4>(a, sq, look_up.at, row[r], vr, s * kStep, c, g, 4 * g, special);
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
                     if (i < live) put_special<HD, 4>(a, place, first_row + i, 16 * j + 4 * g, sum[r].l, special[j]);
             }
-        }
     }
     if (a.splits > 1 && a.arrived) {
         __shared__ int before;
@@ -1163,6 +1129,98 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
         if (last_to_arrive(a, place, before))
             join_rows<HD, T, kThrough>(a, place, first_row, live, join_lanes(a.splits, live, T / (HD / 8)), kValueUnit<FMT>, *reinterpret_cast<JoinSpace<HD, T> *>(&lds));
     }
+}
+
+// The same over a cache held in 4 bits.  A code and its block's power of two make an fp16 number, so that the conversion to fp16 (one instruction for
+// two values, the scale taken in) is all that the format costs, and the rest is as for fp16 rows.  A lane has a quarter of a key's row, which is its share
+// of all of an operand's columns.  Values would need a transposition by codes of half a byte: a lane takes a block of 32 instead, with one scale, and
+// puts it as fp16 where the transposing reads of LDS find it, in its wavefront's own rows, so that no barrier is needed.
+// Bound: few rows as tree_tiles, by the chain of a step's loads (one token over 4096 rows, 32 heads, 10.7 us, 8.9 MB; over 32768 rows, 64 / 8 heads,
+// 15.5 us, 36 MB); many rows by the instructions of a step, 0.76 us of 32 rows x 32 keys x 128 dimensions on a SIMD: conversions, weights and products
+// take their turns there (64 tokens over 8192 rows, 32 / 8 heads, batch 16: 172 to 178 us, 0.8 PFLOP/s; tree_blocks with 4-bit staging the same).
+// Without gain: two or three steps of loads ahead in registers (1.4 us more in short calls: the code is larger) or in LDS, steps of 64 keys (long calls
+// -6 %, short ones +1 us), the next step's scores among this one's weights, 64 rows a wavefront (206 us), three wavefronts a SIMD (176).
+template <int HD, int NR, bool FORMS>
+__global__ __launch_bounds__(NT, 2) void tree_fours(const TreeArgs a)
+{
+    constexpr int FMT = CF_CACHE_MXFP4, KS = HD / 32, NJ = HD / 16, ROW = HD / 2, SROW = HD / kBlock, VROW = 2 * HD + 32;
+    __shared__ union alignas(16) {
+        char values[NW][kStep * VROW];                              // of a wavefront's step
+        TilesSums<HD> sums;
+    } u;
+    __shared__ TilesSpace<HD, NR> space;
+    Lookup<16 * NR> &look_up = space.look_up;
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const Place place(a);
+    if (place.unit >= a.units) return;
+    const Sequence sq(a, place.b);
+    const int first_row = place.block * (16 * NR), live = min(sq.n * a.group - first_row, 16 * NR);
+    if (live <= 0) return;
+
+    h8 q[NR][KS];
+    Row row[NR];
+    int nearest = kFar, farthest = -kFar;                           // of the positions of the block's tokens
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+        row[r] = load_row<HD, FORMS>(a, sq, place, first_row + 16 * r + c, look_up.mask[16 * r + c], q[r], nearest, farthest, [&](int ks) { return Keys4<HD>::dim(ks, g); });
+    if (FORMS && a.window > 0)
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) nearest = min(nearest, __shfl_xor(nearest, s)), farthest = max(farthest, __shfl_xor(farthest, s));
+    const Part<FORMS, kStep> part(a, sq, place, nearest, farthest);
+
+    const size_t slice = (size_t)place.bh * a.max_seq;
+    const __amdgpu_buffer_rsrc_t kr = cf::buffer_of(a.k + slice * ROW, (uint32_t)sq.end * ROW), vr = cf::buffer_of(a.v + slice * ROW, (uint32_t)sq.end * ROW);
+    const __amdgpu_buffer_rsrc_t ksr = cf::buffer_of(reinterpret_cast<const char *>(a.k_scale) + slice * SROW, (uint32_t)sq.end * SROW);
+    const __amdgpu_buffer_rsrc_t vsr = cf::buffer_of(reinterpret_cast<const char *>(a.v_scale) + slice * SROW, (uint32_t)sq.end * SROW);
+    const float to_score = score_factor<HD, FMT>(FORMS ? a.cap : 0.f);
+
+    Keys4<HD> keys;
+    Values4<HD, VROW> vals;
+    Sums<HD> sum[NR];
+    bool careful = false, unfit = false;                            // unfit: NaN were left out of the product
+    int j0 = part.at(wv) * kStep;
+    if (part.has(wv)) {
+        keys.load(kr, ksr, j0, c, g);
+        vals.load(vr, vsr, j0, lane);
+    }
+    if (part.end * kStep > sq.len) {
+        fill<FORMS, NT>(a, sq, first_row, live, look_up);
+        lds_barrier();
+    }
+    for (int i = wv; part.has(i); i += NW) {
+        const bool masked = j0 + kStep > sq.len || j0 < part.all_from;      // (the same for the whole wavefront)
+        const int next = part.at(i + NW) * kStep;
+        // ---- scores
+        f32x4 s[NR][2];
+        keys.settle();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const h8 k = keys.operand(t, ks);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) s[r][t] = mfma16(k, q[r][ks], ks ? s[r][t] : f32x4{0.f, 0.f, 0.f, 0.f});
+            }
+        keys.load(kr, ksr, next, c, g);
+        // ---- values
+        vals.settle();
+        if (masked) unfit = __any(vals.take_out_unfit()) || unfit;
+        vals.store(u.values[wv], lane);
+        vals.load(vr, vsr, next, lane);
+        h8 w[NR];
+        weigh_apart<HD, FMT, FORMS, NR>(a, sq, look_up.at, row, g, j0, masked, careful, to_score, s, sum, w);
+        wave_sync();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const h8 v = transposed<VROW>(u.values[wv], 0, 16 * j, c, g);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) sum[r].acc[j] = mfma16(v, w[r], sum[r].acc[j]);
+        }
+        wave_sync();
+        j0 = next;
+    }
+    __syncthreads();                                                // the sums go where the values were
+    finish_tiles<HD, FMT, NR, FORMS>(a, sq, place, part, first_row, live, vsr, unfit, sum, u.sums, space);
 }
 
 // The parts of a sequence joined by a kernel of its own: as many rows to a workgroup as its threads have.  Bound: memory, behind a launch
@@ -1195,9 +1253,15 @@ struct Shape {
 constexpr Shape kPlain[kShapes] = {{16, 4}, {32, 4}, {64, 8}, {128, 4}, {256, 8}};
 constexpr Shape kPlain8[kShapes] = {{16, 4}, {32, 4}, {32, 4}, {32, 4}, {256, 8}};
 constexpr Shape kForms[kShapes] = {{16, 4}, {16, 4}, {64, 8}, {128, 8}, {128, 8}};
+// 4-bit caches take blocks of 32 rows, with forms of 16, for any number of rows.  (256 rows in eight such blocks against one of tree_blocks: 64 tokens,
+// 8 KV heads, over 4096 rows, batch 1 / 4: 18.9 / 34.3 us against 31.7 / 44.8, over 8192 rows, batch 16: 172 both; with forms, 160 rows over 4096,
+// batch 2: 31.3 us in blocks of 16, 40.3 of 32, 45.9 by tree_blocks.)
+constexpr Shape kPlain4[kShapes] = {{16, 4}, {32, 4}, {32, 4}, {32, 4}, {32, 4}};
+constexpr Shape kForms4[kShapes] = {{16, 4}, {16, 4}, {16, 4}, {16, 4}, {16, 4}};
 
 const Shape (&shapes_of(const cf_cache_config &c, bool forms))[kShapes]
 {
+    if (c.format == CF_CACHE_MXFP4) return forms ? kForms4 : kPlain4;
     return forms ? kForms : c.format == CF_CACHE_F16 ? kPlain : kPlain8;
 }
 
@@ -1214,14 +1278,11 @@ KernelFn pick_shape(int shape)
         return fn[shape];
     }
 }
-// in 4 bits
 template <int HD, bool FORMS>
 KernelFn pick_four(int shape)
 {
-    if constexpr (FORMS)
-        return shape < 2 ? tree_fours<HD, 1, true, 2> : shape == 2 ? tree_blocks<HD, CF_CACHE_MXFP4, 4, 2, 1, true> : tree_blocks<HD, CF_CACHE_MXFP4, 8, 1, 1, true>;
-    else
-        return shape == 0 ? tree_fours<HD, 1, false, 2> : shape < 4 ? tree_fours<HD, 2, false, 2> : tree_blocks<HD, CF_CACHE_MXFP4, 8, 1, 2, false>;
+    if constexpr (FORMS) return tree_fours<HD, 1, true>;
+    else return shape == 0 ? tree_fours<HD, 1, false> : tree_fours<HD, 2, false>;
 }
 template <int HD, bool FORMS>
 KernelFn pick_format(int fmt, int shape)
@@ -1259,8 +1320,9 @@ constexpr int kJoinedInPlace = 10240, kManyInPlace = 16384, kManyBlocks = 32;
 // parts: 2048 rows 8.7 / 8.9 / 9.7 us, 8192 rows 13.1 / 11.3 / 12.3.)  The join kernel costs about the same for any number: three times as
 // many keys under the root.  (One token, 64 heads, fp16, 4096 rows: 12 / 16 / 24 / 32 parts 11.7 / 11.5 / 10.6 / 10.5.)  Scores with forms take
 // twice the time per key.  No more parts than leave every workgroup a compute unit (280 workgroups on 256 units 16.0 us, 252 13.7: 16 tokens over
-// 4096 rows with forms, 14 / 7 heads, batch 2), or, where parts then still have 1024 keys, than fill the eight wavefronts that a unit
-// holds (32 tokens over 8192 int8 rows, batch 4, 2 / 4 parts 37.6 / 32.5 us; 64 tokens over 4096 e4m3 rows, 32 heads, 4 / 8 parts
+// 4096 rows with forms, 14 / 7 heads, batch 2), or, where parts then still have 1024 keys (512 in 4 bits and blocks of 16 rows: one token over 32768
+// rows, 8 KV heads, 32 / 64 parts 16.8 / 15.6 us; 64 tokens over 4096, blocks of 32, 4 / 8 parts 18.9 / 21.7), than fill the eight wavefronts that a
+// unit holds (32 tokens over 8192 int8 rows, batch 4, 2 / 4 parts 37.6 / 32.5 us; 64 tokens over 4096 e4m3 rows, 32 heads, 4 / 8 parts
 // 17.7 / 20.6).  Never fewer than 128 keys, and one part up to 384 keys (192 with forms) where a workgroup has at most 64 rows: nothing to
 // join saves 0.7 to 1.7 us.  Parts are whole multiples of 128 keys, so that all wavefronts have as many steps.
 Plan plan_of(const cf_cache_config &c, bool forms, int batch, int tokens, int keys, int cus, int limit)
@@ -1283,7 +1345,8 @@ Plan plan_of(const cf_cache_config &c, bool forms, int batch, int tokens, int ke
     const double work = forms ? 2.0 * keys : keys;
     int few = in_rounds(most / std::sqrt(work / 24) + 0.5);
     if (!in_place(few)) few = in_rounds(most / std::sqrt(work / 8));
-    const int wanted = keys / 1024 < few ? few : keys / 1024 < full ? keys / 1024 : full;
+    const int long_parts = keys / (c.format == CF_CACHE_MXFP4 && shape.rows == 16 ? 512 : 1024);
+    const int wanted = long_parts < few ? few : long_parts < full ? long_parts : full;
     p.splits = work <= 384 && shape.rows <= 64 ? 1 : std::min(wanted, most);
     if (p.splits > kMaxSplits) p.splits = kMaxSplits;
     if (limit > 0) p.splits = p.splits > limit ? limit : p.splits;

@@ -169,30 +169,37 @@ struct Values {
     }
 };
 
-// ---- 4-bit rows. Both operands are exact fp16 values: the conversions take the block's scale in, one instruction for two values.
+// ---- 4-bit rows.  Both operands are exact fp16 values: the conversions take the block's scale in, one instruction for two values.
 
-// The keys of a step: a quarter of a row (one block of 128 dimensions, half of one of 64) and its scale to a lane.
+// The keys of a step of 32: a quarter of a row (one block of 128 dimensions, half of one of 64) and its scale to a lane.
 template <int HD>
 struct Keys4 {
     static constexpr int ROW = HD / 2, WORDS = HD / 32, SROW = HD / cache::kBlock;      // bytes of a row; dwords of a quarter; scales of a row
     uint32_t raw[2][WORDS];
-    uint32_t scale[2];
+    uint16_t scale[2];
     static __device__ __forceinline__ int dim(int ks, int g) { return HD / 4 * g + 8 * ks; }
     __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t sr, int j0, int c, int g)
     {
+        const uint32_t rows = (uint32_t)j0 * ROW + (c * ROW + 4 * WORDS * g), scales = (uint32_t)j0 * SROW + (c * SROW + g * SROW / 4);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const uint32_t off = (j0 + 16 * t + c) * ROW + 4 * WORDS * g;
             if constexpr (WORDS == 4) {
-                const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+                const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, rows + 16 * t * ROW, 0, 0));
 #pragma unroll
                 for (int w = 0; w < 4; ++w) raw[t][w] = x[w];
             } else {
-                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, rows + 16 * t * ROW, 0, 0));
                 raw[t][0] = x[0], raw[t][1] = x[1];
             }
-            scale[t] = __builtin_amdgcn_raw_buffer_load_b8(sr, (j0 + 16 * t + c) * SROW + g * SROW / 4, 0, 0);
+            scale[t] = __builtin_amdgcn_raw_buffer_load_b8(sr, scales + 16 * t * SROW, 0, 0);
         }
+    }
+    // Once before the operands.  (What is made of loaded registers would else be moved to the end of the step before, behind the loads, and wait
+    // for them there: the scales' extension to 32 bits alone did, so that they are carried in 16.)
+    __device__ __forceinline__ void settle()
+    {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) asm volatile("" : "+v"(scale[t]));
     }
     __device__ __forceinline__ h8 operand(int t, int ks) const
     {
@@ -200,47 +207,49 @@ struct Keys4 {
     }
 };
 
-// The values of a step: NJ adjacent dimensions of eight rows to a lane, converted two dimensions at a time and then transposed.
-template <int HD>
+// The values of a step of 32: 32 adjacent values of a row and their scale to a lane and load; they go through LDS as fp16 (rows of VROW bytes, for
+// transposing reads).
+template <int HD, int VROW>
 struct Values4 {
-    static constexpr int NJ = HD / 16, ROW = HD / 2, SROW = HD / cache::kBlock;
-    uint32_t raw[8], scale[8];
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t sr, int j0, int c, int g)
+    static constexpr int ROW = HD / 2, SROW = HD / cache::kBlock, LOADS = HD / 64, ROWS = 64 / SROW;     // ROWS of a load
+    u32x4 raw[LOADS];
+    uint16_t scale[LOADS];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t sr, int j0, int lane)
     {
+        const uint32_t blocks = (uint32_t)j0 * SROW + lane;         // (a block has 16 bytes of codes)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const uint32_t row = j0 + 4 * g + (u < 4 ? u : 12 + u);
-            if constexpr (NJ == 8)
-                raw[u] = __builtin_amdgcn_raw_buffer_load_b32(r, row * ROW + 4 * c, 0, 0);
-            else
-                raw[u] = __builtin_amdgcn_raw_buffer_load_b16(r, row * ROW + 2 * c, 0, 0);
-            scale[u] = __builtin_amdgcn_raw_buffer_load_b8(sr, row * SROW + NJ * c / cache::kBlock, 0, 0);
+        for (int i = 0; i < LOADS; ++i) {
+            raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, 16 * blocks + 1024 * i, 0, 0));
+            scale[i] = __builtin_amdgcn_raw_buffer_load_b8(sr, blocks + 64 * i, 0, 0);
         }
     }
-    // the operands of dimensions NJ c + 2 PAIR and NJ c + 2 PAIR + 1
-    template <int PAIR>
-    __device__ __forceinline__ void operands(h8 (&f)[2]) const
+    // once before what follows, as for the keys
+    __device__ __forceinline__ void settle()
     {
-        u32x4 o[2];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[2 * w], cache::scale_of_byte(scale[2 * w]), PAIR));
-            const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(raw[2 * w + 1], cache::scale_of_byte(scale[2 * w + 1]), PAIR));
-            o[0][w] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
-            o[1][w] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-        }
-        f[0] = __builtin_bit_cast(h8, o[0]), f[1] = __builtin_bit_cast(h8, o[1]);
+        for (int i = 0; i < LOADS; ++i) asm volatile("" : "+v"(scale[i]));
     }
     // Takes NaN blocks out (their values count as zeros); not 0 if there were some.
     __device__ __forceinline__ uint32_t take_out_unfit()
     {
         uint32_t odd = 0;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            odd |= scale[u] == 255u;
-            scale[u] = scale[u] == 255u ? 0u : scale[u];
+        for (int i = 0; i < LOADS; ++i) {
+            odd |= scale[i] == 255;
+            scale[i] = scale[i] == 255 ? 0 : scale[i];
         }
         return odd;
+    }
+    __device__ __forceinline__ void store(char *to, int lane) const
+    {
+        // chunk 4 col + w at chunk_at of it: the pairs of columns 2 and 3 change places
+        const int col = lane % SROW, swap = HD == 128 ? 16 * (col >> 1) : 0;
+        char *first = to + lane / SROW * VROW + 64 * col, *even = first + swap, *odd = first - swap;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                *reinterpret_cast<u32x4 *>((w & 1 ? odd : even) + ROWS * VROW * i + 16 * w) = cache::block_values(raw[i][w], cache::scale_of_byte(scale[i]));
     }
 };
 
