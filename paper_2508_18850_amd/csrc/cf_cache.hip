@@ -7,6 +7,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 namespace {
 
@@ -24,9 +25,12 @@ constexpr int kMaxKept = 256;      // tokens of a cf_cache_keep: their rows are 
 // Arithmetic: angle, cos, sin and the rotation are fp64 and the result is rounded to fp16 once.  A fp32 rotation is off by 2^-23, which
 // moves one value in some thousands to the other fp16 neighbour, and through it one 8-bit code in 10^5; in fp64 the angle is off by some
 // 2^-51 of itself (a power, the product of two, the product with the position), at position 32768 by 2^-36, which moves one value in
-// 10^7; the vector units are idle beside it all the same (27.6 million instructions of 16384 wavefronts in 70 us).
-// Bound: memory.  Two prompts of 8192 and 6144 tokens, 32 + 2 x 8 heads of 128 dimensions, into int8: 324 MB in 70 us, 4.6 TB/s (a copy
-// reaches 4.8).  With few tokens the launch: one token 3.6 us on the GPU, so its heads are spread over more workgroups.
+// 10^7; beside memory it costs little where the rarer steps of the roundings are left out (halves_once; two prompts of 4096 tokens, 32 + 2 x 8 heads
+// of 128 dimensions, with norms, into fp16: 44.9 us, 57 with all steps for every value and the weights multiplied in head by head).
+// With norms (cf_cache_append_normed) every head's row is divided by the root of its mean square, in fp64 too: the squares of fp16 values are exact.
+// The weights are multiplied into cos and sin, once for a token and not for each head; a row's norm is common to the pair, so that it comes last.
+// Bound: memory; the next heads' rows are requested before these are used (without it 4 % more).  Those prompts: 202 MB in 44.9 us, 4.5 TB/s (a copy
+// reaches 5.1); into 4 bits, 177 MB, 40.5 us, 4.4 TB/s.  With few tokens the launch: one token 3.6 us on the GPU, so its heads are spread over more workgroups.
 struct AppendArgs {
     const uint16_t *qkv;
     uint16_t *q_out;
@@ -51,6 +55,22 @@ __device__ __forceinline__ _Float16 half_once(double x)
     uint32_t bits = __builtin_bit_cast(uint32_t, f);
     if ((rest > 0.0 || rest < 0.0) && !(bits & 1u) && f != 0.f) bits += (rest > 0.0) == (f > 0.f) ? 1u : ~0u;
     return (_Float16)__builtin_bit_cast(float, bits);
+}
+// The same of N at once.  Rounding twice can only matter where the fp32 value is a middle of two fp16 numbers, and then (or with any other middle
+// that fp16's small numbers have) at least its last twelve bits are 0: one value in 4096, else the conversions alone.
+template <int N>
+__device__ __forceinline__ void halves_once(const double (&x)[N], _Float16 (&h)[N])
+{
+    uint32_t least = ~0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float f = (float)x[i];
+        least = min(least, __builtin_bit_cast(uint32_t, f) & 0xfffu);
+        h[i] = (_Float16)f;
+    }
+    if (__any(least == 0))
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] = half_once(x[i]);
 }
 
 template <int HD>
@@ -98,22 +118,42 @@ __device__ __forceinline__ double row_norm(const h8 &lo, const h8 &hi, double ep
     return m == (double)INFINITY ? 0.0 : r;
 }
 
+// The pair (x, y) of a rotation becomes (x xx - y yx, y yy + x xy): cos, sin, cos, sin, with norms each times the weight of what it is multiplied by.
+struct alignas(16) Turn {
+    double xx, yx;
+};
+struct alignas(16) WeightedTurn {
+    double xx, yx, yy, xy;
+};
 template <int HD, int FMT, bool NORM>
 __global__ __launch_bounds__(NT) void cache_append(const AppendArgs a)
 {
-    constexpr int LPR = HD / 16, RPW = 64 / LPR, HALF = HD / 2;
-    __shared__ double2 turn[4][HALF];
+    constexpr int LPR = HD / 16, RPW = 64 / LPR, HALF = HD / 2, KINDS = NORM ? 2 : 1;
+    // of a token's pair 8 i + j at j LPR + i, so that the lanes of a row read adjacent ones; with norms for queries and for keys
+    __shared__ std::conditional_t<NORM, WeightedTurn, Turn> turn[4][KINDS][HALF];
     const int tid = threadIdx.x, wv = tid >> 6, lane = tid & 63;
     const int b = blockIdx.z, t0 = blockIdx.x * a.nt;
     const int n = a.rows.fresh(b), len = a.rows.cached(b);
     if (t0 >= n) return;
     {
-        const int slot = tid / 64, i = lane;
+        const int slot = tid / 64, i = lane, at = i % 8 * LPR + i / 8;
         if (slot < a.nt && i < HALF && t0 + slot < n) {
             const int depth = a.depth ? a.depth[(size_t)b * a.depth_stride + t0 + slot] : t0 + slot;
             double c, s;
-            cf::rope_cos_sin64((double)len + (double)depth, a.theta[i], c, s);
-            turn[slot][i] = make_double2(c, s);
+            if constexpr (NORM) {
+                double w[2][2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint16_t *of = k ? a.k_weight : a.q_weight;
+                    w[k][0] = (double)(float)__builtin_bit_cast(_Float16, of[i]), w[k][1] = (double)(float)__builtin_bit_cast(_Float16, of[i + HALF]);
+                }
+                cf::rope_cos_sin64((double)len + (double)depth, a.theta[i], c, s);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) turn[slot][k][at] = {c * w[k][0], s * w[k][1], c * w[k][1], s * w[k][0]};
+            } else {
+                cf::rope_cos_sin64((double)len + (double)depth, a.theta[i], c, s);
+                turn[slot][0][at] = {c, s};
+            }
         }
     }
     __syncthreads();
@@ -121,26 +161,42 @@ __global__ __launch_bounds__(NT) void cache_append(const AppendArgs a)
     if (t >= n) return;
     const int H = a.nq + 2 * a.nkv, groups = (H + RPW - 1) / RPW, step = (NW / a.nt) * gridDim.y;
     const int li = lane % LPR;
-    for (int grp = wv / a.nt + (NW / a.nt) * blockIdx.y; grp < groups; grp += step) {
+    const uint16_t *src = a.qkv + ((size_t)b * a.rows.tokens + t) * H * HD + 8 * li;
+    int grp = wv / a.nt + (NW / a.nt) * blockIdx.y;
+    h8 next_lo = {}, next_hi = {};
+    auto load = [&](int of) {
+        const int head = of * RPW + lane / LPR;
+        if (head < H) next_lo = *reinterpret_cast<const h8 *>(src + (size_t)head * HD), next_hi = *reinterpret_cast<const h8 *>(src + (size_t)head * HD + HALF);
+    };
+    load(grp);
+    for (; grp < groups; grp += step) {
         const int head = grp * RPW + lane / LPR;
+        h8 lo = next_lo, hi = next_hi;
+        load(grp + step);
         if (head >= H) continue;                                   // (whole rows of lanes: the maxima below stay inside a row)
-        const uint16_t *src = a.qkv + (((size_t)b * a.rows.tokens + t) * H + head) * HD + 8 * li;
-        h8 lo = *reinterpret_cast<const h8 *>(src), hi = *reinterpret_cast<const h8 *>(src + HALF);
         if (head < a.nq + a.nkv) {
-            h8 wlo, whi;
+            const auto *turns = turn[slot][NORM && head >= a.nq] + li;
             double r = 1.0;
-            if constexpr (NORM) {
-                const uint16_t *w = (head < a.nq ? a.q_weight : a.k_weight) + 8 * li;
-                wlo = *reinterpret_cast<const h8 *>(w), whi = *reinterpret_cast<const h8 *>(w + HALF);
-                r = row_norm<HD>(lo, hi, a.eps);
-            }
+            if constexpr (NORM) r = row_norm<HD>(lo, hi, a.eps);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const double2 cs = turn[slot][8 * li + j];
-                double x = (double)(float)lo[j], y = (double)(float)hi[j];
-                if constexpr (NORM) x *= (double)(float)wlo[j] * r, y *= (double)(float)whi[j] * r;
-                lo[j] = half_once(x * cs.x - y * cs.y);
-                hi[j] = half_once(y * cs.x + x * cs.y);
+            for (int j0 = 0; j0 < 8; j0 += 2) {
+                double z[4];
+                _Float16 h[4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const auto cs = turns[(j0 + j) * LPR];
+                    const double x = (double)(float)lo[j0 + j], y = (double)(float)hi[j0 + j];
+                    if constexpr (NORM) {
+                        z[j] = (x * cs.xx - y * cs.yx) * r;
+                        z[2 + j] = (y * cs.yy + x * cs.xy) * r;
+                    } else {
+                        z[j] = x * cs.xx - y * cs.yx;
+                        z[2 + j] = y * cs.xx + x * cs.yx;
+                    }
+                }
+                halves_once(z, h);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) lo[j0 + j] = h[j], hi[j0 + j] = h[2 + j];
             }
         }
         if (head < a.nq) {
