@@ -562,9 +562,9 @@ int64_t cf_tree_algorithmic_bytes(const cf_tree_config *cfg, int32_t batch, int3
  * cf_linear_forward: x [rows, n_in], x_scale [rows], W [n_out, n_in] (row n: the weights into output n), w_scale [n_out] read; out [rows,
  *   n_out] fp16 fully overwritten.  Codes may have any value from -128 on.  CF_EINVAL: null or misaligned pointers, rows outside
  *   1..max_rows, out overlapping an input, another current device than the handle's.
- * The same inputs give the same bits.  cf_linear_quantize and cf_linear_forward are asynchronous on `stream`, allocate nothing and can be
- * captured and replayed.  A handle must not be used from two streams at the same time, nor two captured graphs with calls on one handle replayed
- * at the same time.
+ * The same inputs give the same bits, also among other rows or in a call with more or fewer of them.  cf_linear_quantize and cf_linear_forward are
+ * asynchronous on `stream`, allocate nothing and can be captured and replayed.  A handle has no workspace: it may be used from several streams,
+ * and by graphs that are replayed, at the same time.
  */
 typedef struct cf_linear_config {
     int32_t n_in, n_out, max_rows;

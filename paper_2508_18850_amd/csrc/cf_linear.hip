@@ -181,8 +181,9 @@ __global__ __launch_bounds__(64 * WAVES) void linear_stream(const LinearArgs a)
 }
 
 // Many rows: WM x WN wavefronts share a tile of BM rows by BN outputs.  Steps of 128 codes go from memory straight into LDS, one step ahead of the
-// one that is used.  A row's eight 16-byte chunks lie there at places chunk ^ (row & 7), so that the rows of an operand are read from different banks;
-// the loads fill LDS in the order of the lanes, so it is their addresses in memory that are permuted.
+// one that is used.  A row's eight 16-byte chunks lie there at places chunk ^ (row / 2 & 7), so that the rows of an operand are read from different banks
+// (chunk ^ (row & 7): every read from twice as many cycles); the loads fill LDS in the order of the lanes, so it is their addresses in memory that
+// are permuted.
 // Operands of a 32 x 32 x 32 step, lane = 32 g + c: row c, codes 16 g .. 16 g + 15; the result: output 8 (r / 4) + 4 g + r % 4 of row c.
 constexpr int kTileStep = 128;
 template <int BM, int BN, int WM, int WN, int STAGES>
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tiles(const LinearArgs a)
 {
     constexpr int WAVES = WM * WN, T = 64 * WAVES, TM = BM / WM / 32, TN = BN / WN / 32, XL = BM / 8 / WAVES, WL = BN / 8 / WAVES, PITCH = 2 * BN + 16;
     constexpr int STAGE = (BM + BN) * kTileStep, SPACE = STAGES * STAGE > BM * PITCH ? STAGES * STAGE : BM * PITCH;
-    static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "whole loads");
+    static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && WAVES % 2 == 0, "whole loads, of row blocks of 8 whose number is odd where the wavefront's is");
     __shared__ alignas(16) char lds[SPACE];
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, g = lane >> 5;
     // each die takes a part of the tiles, eight row blocks by as many output blocks as it has room for at a time
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tiles(const LinearArgs a)
     }
     const int m0 = m_block * BM, n0 = n_block * BN, rows = min(BM, a.rows - m0), cols = min(BN, a.n_out - n0);
     const __amdgpu_buffer_rsrc_t xr = cf::buffer_of(a.x + (size_t)m0 * a.n_in, (uint32_t)rows * a.n_in), wr = cf::buffer_of(a.w + (size_t)n0 * a.n_in, (uint32_t)cols * a.n_in);
-    const int chunk = (lane & 7) ^ (lane >> 3);
+    const int chunk = (lane & 7) ^ (4 * (wv & 1) + (lane >> 4));
     uint32_t x_at[XL], w_at[WL];                                    // rows that are not there repeat the last one
 #pragma unroll
     for (int i = 0; i < XL; ++i) x_at[i] = min(8 * (wv + WAVES * i) + (lane >> 3), rows - 1) * a.n_in + 16 * chunk;
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tiles(const LinearArgs a)
         const int end = a.n_in - turned(i) * kTileStep;
         if (end < kTileStep) {                                      // what lies behind the end of the sums counts as zeros
             for (int e = tid; e < BN * 8; e += T)
-                if (16 * (e & 7) >= end) *reinterpret_cast<i32x4 *>(now + BM * kTileStep + (e >> 3) * kTileStep + 16 * ((e ^ e >> 3) & 7)) = i32x4{0, 0, 0, 0};
+                if (16 * (e & 7) >= end) *reinterpret_cast<i32x4 *>(now + BM * kTileStep + (e >> 3) * kTileStep + 16 * ((e ^ e >> 4) & 7)) = i32x4{0, 0, 0, 0};
             cf_lds_barrier();
         }
         next = now;
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tiles(const LinearArgs a)
         // operands are read a product ahead
         i32x4 x[2][TM], w[2][TN];
         auto read = [&](int kk) {
-            const int place = 16 * ((2 * kk + g) ^ (c & 7));
+            const int place = 16 * ((2 * kk + g) ^ (c >> 1 & 7));
 #pragma unroll
             for (int j = 0; j < TN; ++j) w[kk & 1][j] = *reinterpret_cast<const i32x4 *>(ws + (my_n + 32 * j + c) * kTileStep + place);
 #pragma unroll
