@@ -190,9 +190,10 @@ __global__ __launch_bounds__(64 * WAVES) void linear_stream(const LinearArgs a)
 // (chunk ^ (row & 7): every read from twice as many cycles); the loads fill LDS in the order of the lanes, so it is their addresses in memory that
 // are permuted.
 // Bound: the matrix units, and behind them the power that the card has for them: 8192 x 8192 -> 10240 in 604 us, 2.28 Pop/s, the units busy for 64 % of
-// the cycles at 1.7 GHz (a library's product of these sizes 647 us).  256 x 4096 -> 6144 takes 17.1 us, 512 x 4096 -> 4096 17.2: start, steps
+// the cycles at 1.7 GHz (a library's product of these sizes 647 us; the products alone, of operands that are not loaded, 475; the loads and the reading of
+// operands alone 396).  256 x 4096 -> 6144 takes 17.1 us, 512 x 4096 -> 4096 17.2: start, steps
 // and end of one tile on a compute unit.  Without gain: 128 x 128 to a wavefront, four on a compute unit (649 us); operands read where the compiler puts
-// them (618); through registers in place of direct loads (slower at all sizes).
+// them (618); the barrier and the next step's first operands before the last product of a step (609); through registers in place of direct loads (slower at all sizes).
 // Operands of a 32 x 32 x 32 step, lane = 32 g + c: row c, codes 16 g .. 16 g + 15; the result: output 8 (r / 4) + 4 g + r % 4 of row c.
 constexpr int kTileStep = 128;
 template <int BM, int BN, int WM, int WN, int STAGES>

@@ -208,6 +208,33 @@ def test_two_handles_on_two_streams():
         assert torch.equal(c.out[:64], w)
 
 
+def test_one_handle_on_two_streams():
+    """It has no workspace: two streams, and two graphs with calls on it, at the same time."""
+    cases = [Product(16, 4096, 512, seed=i) for i in range(2)]
+    want = [c.check() for c in cases]
+    cases[1].linear = cases[0].linear
+    streams = [torch.cuda.Stream() for _ in cases]
+    graphs = [torch.cuda.CUDAGraph() for _ in cases]
+    for c, g in zip(cases, graphs):
+        with torch.cuda.graph(g):
+            for _ in range(4):
+                c.call(torch.cuda.current_stream().cuda_stream)
+    for replayed in (False, True):
+        for c in cases:
+            c.out.fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for c, s, g in zip(cases, streams, graphs):
+                if replayed:
+                    with torch.cuda.stream(s):
+                        g.replay()
+                else:
+                    c.call(s.cuda_stream)
+        torch.cuda.synchronize()
+        for c, w in zip(cases, want):
+            assert torch.equal(c.out[:len(w)], w), replayed
+
+
 def test_offsets_beyond_32_bits():
     """Codes and results of more than 4 GiB; the last rows against a product of their own."""
     M, K, N = 300000, 16384, 8192
