@@ -2,9 +2,9 @@
 #include "../../include/cfdecode.h"
 #include "cf_cache_device.h"
 #include "cf_lanes_device.h"
+#include "cf_linear_plan.h"
 #include "cf_stream_device.h"
 
-#include <algorithm>
 #include <cstring>
 #include <new>
 
@@ -105,8 +105,8 @@ __global__ __launch_bounds__(64 * WAVES) void linear_stream(const LinearArgs a)
     constexpr int RING = DEPTH * PLACE, SUMS = ROWS * PITCH * 4, SPACE = WAVES * (RING > SUMS ? RING : SUMS);
     __shared__ alignas(16) char lds[SPACE];
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
-    // the row blocks of the same outputs follow each other on one die
-    const int turn = blockIdx.x >> 3, n_block = turn / a.row_blocks * 8 + (blockIdx.x & 7), m0 = (turn % a.row_blocks) * ROWS, n0 = n_block * COLS;
+    const cf::linear::Block mine = cf::linear::stream_block(blockIdx.x, a.row_blocks, a.col_blocks);
+    const int m0 = mine.m * ROWS, n_block = mine.n, n0 = n_block * COLS;
     if (n0 >= a.n_out) return;
     const int rows = min(ROWS, a.rows - m0), cols = min(COLS, a.n_out - n0);
     const __amdgpu_buffer_rsrc_t xr = cf::buffer_of(a.x + (size_t)m0 * a.n_in, (uint32_t)rows * a.n_in), wr = cf::buffer_of(a.w + (size_t)n0 * a.n_in, (uint32_t)cols * a.n_in);
@@ -298,33 +298,12 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_tiles(const LinearArgs a)
     }
 }
 
-// The ways to divide a product.  What a step of 128 codes of the sum takes a workgroup that has a compute unit for itself, and one among others on it, in
-// us; a call takes about 3 us more.  (Measured at 4096 to 11008 codes and 1 to 8192 rows, all ways at each; a wavefront of the tiles waits for its
-// operands and multiplies by turns, so that a step of a tile that is alone takes 1.5 times as long as the matrix units need for it or more.)
-struct Way {
-    void (*kernel)(const LinearArgs);
-    int rows, cols, threads;       // of a workgroup
-    bool tiles;
-    float alone, among;
+using Kernel = void (*)(const LinearArgs);
+constexpr Kernel kKernels[] = {            // of cf::linear::kWays
+    linear_stream<1, 1, 4, 3>, linear_stream<1, 2, 4, 4>, linear_stream<2, 2, 4, 2>, linear_stream<4, 2, 4, 2>, linear_stream<4, 4, 4, 2>,
+    linear_tiles<64, 64, 2, 2, 4>, linear_tiles<128, 64, 2, 2, 4>, linear_tiles<256, 128, 4, 2, 3>, linear_tiles<256, 256, 2, 4, 2>,
 };
-constexpr Way kWays[] = {
-    {linear_stream<1, 1, 4, 3>, 16, 16, 256, false, 0.085f, 0.087f}, {linear_stream<1, 2, 4, 4>, 16, 32, 256, false, 0.145f, 0.16f},
-    {linear_stream<2, 2, 4, 2>, 32, 32, 256, false, 0.17f, 0.145f},  {linear_stream<4, 2, 4, 2>, 64, 32, 256, false, 0.23f, 0.23f},
-    {linear_stream<4, 4, 4, 2>, 64, 64, 256, false, 0.27f, 0.28f},   {linear_tiles<64, 64, 2, 2, 4>, 64, 64, 256, true, 0.31f, 0.26f},
-    {linear_tiles<128, 64, 2, 2, 4>, 128, 64, 256, true, 0.42f, 0.44f}, {linear_tiles<256, 128, 4, 2, 3>, 256, 128, 512, true, 1.0f, 1.11f},
-    {linear_tiles<256, 256, 2, 4, 2>, 256, 256, 512, true, 1.5f, 1.87f},
-};
-const Way &way_of(const cf_linear_config &c, int rows, int cus)
-{
-    const Way *best = kWays;
-    double least = 0;
-    for (const Way &w : kWays) {
-        const long long workgroups = (long long)((rows + w.rows - 1) / w.rows) * ((c.n_out + w.cols - 1) / w.cols), on_one = (workgroups + cus - 1) / cus;
-        const double step = on_one == 1 && workgroups * 4 <= cus * 3 ? w.alone : std::max(w.alone, (float)on_one * w.among);
-        if (&w == kWays || step < least) best = &w, least = step;
-    }
-    return *best;
-}
+static_assert(sizeof kKernels / sizeof *kKernels == cf::linear::kNumWays, "a kernel for each way");
 
 constexpr int kMostRows = 1 << 23;         // workgroups of a launch
 constexpr int kMostIn = 131056;            // 128^2 times as many is below 2^31
@@ -401,11 +380,11 @@ int cf_linear_forward(cf_linear t, int32_t rows, const int8_t *x, const float *x
     if (hipGetDevice(&dev) != hipSuccess) return CF_EHIP;
     if (dev != t->device) return CF_EINVAL;
     LinearArgs a = {x, W, x_scale, w_scale, static_cast<uint16_t *>(out), rows, c.n_in, c.n_out, 0, 0};
-    const Way &p = way_of(c, rows, t->cus);
-    a.row_blocks = (rows + p.rows - 1) / p.rows, a.col_blocks = (c.n_out + p.cols - 1) / p.cols;
-    const int units = p.tiles ? a.row_blocks * a.col_blocks : a.col_blocks;
-    const unsigned grid = (units + 7) / 8 * 8 * (p.tiles ? 1 : a.row_blocks);
-    hipLaunchKernelGGL(p.kernel, dim3(grid), dim3(p.threads), 0, static_cast<hipStream_t>(stream), a);
+    const int way = cf::linear::way_of(c.n_out, rows, t->cus);
+    const cf::linear::Way &p = cf::linear::kWays[way];
+    a.row_blocks = cf::linear::blocks_of(rows, p.rows), a.col_blocks = cf::linear::blocks_of(c.n_out, p.cols);
+    const unsigned grid = p.tiles ? (unsigned)(a.row_blocks * a.col_blocks + 7) / 8 * 8 : cf::linear::stream_grid(a.row_blocks, a.col_blocks);
+    hipLaunchKernelGGL(kKernels[way], dim3(grid), dim3(p.threads), 0, static_cast<hipStream_t>(stream), a);
     return hipGetLastError() == hipSuccess ? CF_OK : CF_EHIP;
 }
 
