@@ -50,3 +50,7 @@ def stream_blocks(row_blocks, col_blocks):
 NARROW = [(300, 1376, 136, Way(16, 16, False)), (2001, 208, 8, Way(16, 16, False)), (1000, 1376, 72, Way(16, 32, False)), (1000, 1376, 136, Way(32, 32, False)),
           (2050, 2064, 72, Way(32, 32, False)), (4100, 1376, 72, Way(64, 32, False)), (8200, 496, 24, Way(64, 32, False)), (4100, 1376, 136, Way(64, 64, False)),
           (1000, 1376, 520, Way(64, 64, False)), (8200, 208, 136, Way(128, 64, True))]
+
+# Products that are divided into tiles, likewise: rows, sums and outputs that end inside a tile.
+TILED = [(1000, 1376, 2056, Way(64, 64, True)), (500, 1376, 6152, Way(128, 64, True)), (3000, 1376, 1800, Way(256, 128, True)), (2049, 1376, 4104, Way(256, 256, True)),
+         (4100, 2064, 10248, Way(256, 256, True))]

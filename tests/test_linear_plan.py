@@ -33,3 +33,13 @@ def test_the_row_blocks_of_an_output_follow_each_other(row_blocks, col_blocks):
 def test_ways_of_few_outputs(rows, n_in, n_out, way):
     """What the products of test_gpu_linear_ways.py are divided into, on 256 compute units."""
     assert linear_plan.way_of(rows, n_out) == way and -(-n_out // way.cols) % 8 and rows % way.rows and n_out % way.cols and n_in % 128
+
+
+@pytest.mark.parametrize("rows,n_in,n_out,way", linear_plan.TILED, ids=str)
+def test_ways_of_tiles(rows, n_in, n_out, way):
+    """The same, and more steps than a tile has requested at a time, the short one not the last of all dies (each starts at a step of its own)."""
+    assert linear_plan.way_of(rows, n_out) == way and rows % way.rows and n_out % way.cols and n_in % 128 and -(-n_in // 128) > 8
+
+
+def test_every_way_is_tested():
+    assert {w for *_, w in linear_plan.NARROW + linear_plan.TILED} == set(linear_plan.ways())
