@@ -334,14 +334,16 @@ __global__ __launch_bounds__(NT) void cache_keep(const KeepArgs a)
         const int from = min(max(kept[e / per], 0), n - 1);
         *reinterpret_cast<u32x4 *>(held + 16 * e) = *reinterpret_cast<const u32x4 *>(rows + (size_t)from * a.row_bytes + 16 * (e % per));
     }
-    const int mine = tid < moved ? min(max(kept[tid], 0), n - 1) : 0;
+    const bool scales = a.scale_bytes != 0 && tid < moved;         // (without them nothing more is read before the barrier)
     uint32_t own_scale = 0;
-    if (tid < moved && a.scale_bytes == 4) own_scale = reinterpret_cast<const uint32_t *>(scale)[mine];
-    if (tid < moved && a.scale_bytes == 2) own_scale = reinterpret_cast<const uint16_t *>(scale)[mine];
+    if (scales) {
+        const int mine = min(max(kept[tid], 0), n - 1);
+        own_scale = a.scale_bytes == 4 ? reinterpret_cast<const uint32_t *>(scale)[mine] : reinterpret_cast<const uint16_t *>(scale)[mine];
+    }
     __syncthreads();
     for (int e = tid; e < moved * per; e += NT) *reinterpret_cast<u32x4 *>(rows + 16 * (size_t)e) = *reinterpret_cast<const u32x4 *>(held + 16 * e);
-    if (tid < moved && a.scale_bytes == 4) reinterpret_cast<uint32_t *>(scale)[tid] = own_scale;
-    if (tid < moved && a.scale_bytes == 2) reinterpret_cast<uint16_t *>(scale)[tid] = (uint16_t)own_scale;
+    if (scales && a.scale_bytes == 4) reinterpret_cast<uint32_t *>(scale)[tid] = own_scale;
+    if (scales && a.scale_bytes == 2) reinterpret_cast<uint16_t *>(scale)[tid] = (uint16_t)own_scale;
 }
 static_assert(kMaxKept <= NT, "a thread per scale");
 
