@@ -485,8 +485,8 @@ typedef struct cf_draft {
  *   fp16, 16-byte aligned, for all heads); norm and rotation in fp64, one rounding to fp16.  CF_EINVAL for eps < 0 or not finite, and for weights
  *   that overlap q_out or the cache.  (With eps 0 a head of zeros becomes NaN.)
  * cf_cache_read: rows first .. first + rows - 1 of every head's slice as fp16, k_out and v_out [batch, n_kv, rows, head_dim]; 8-bit
- *   values are rounded once more, from the fp32 product code * scale (4-bit ones are fp16 numbers).  rows 0 does nothing.  k_out, v_out and the cache must not
- *   overlap each other.
+ *   values are rounded once more, from the fp32 product code * scale (4-bit ones are fp16 numbers).  rows 0 does nothing, with valid pointers all the same.  k_out, v_out
+ *   and the cache must not overlap each other.
  * cf_cache_keep: after verification, row row_len[b] + i of every head's slice becomes what row row_len[b] + kept[b][i] was, for
  *   i < n_kept[b] (keys, values and scales; all rows are read before one is written); the rows behind stay as they were.  kept: DEVICE [batch,
  *   tokens] int32, entries clamped into 0..n_b - 1; they may come in any order and more than once; n_kept: DEVICE [batch] int32,
@@ -555,7 +555,7 @@ int64_t cf_tree_algorithmic_bytes(const cf_tree_config *cfg, int32_t batch, int3
  * cf_linear_quantize: x [rows, n] fp16 read, codes [rows, n] and scale [rows] written; the codes are those of CF_CACHE_INT8, correctly rounded: a
  *   row of zeros has scale 0 and codes 0, a row that holds an infinity or a NaN scale NaN and codes 0 (and all of its product is NaN).
  *   CF_EINVAL: rows below 0, n not a positive multiple of 16, null or misaligned pointers, buffers that overlap; CF_EUNSUPPORTED: more than 2^23
- *   rows.  rows 0 does nothing.
+ *   rows.  rows 0 does nothing, with valid pointers all the same (a null one is CF_EINVAL as in any call).
  * cf_linear_create: a handle on the current device for products of up to max_rows rows with weights of this shape (synchronous).
  *   CF_EINVAL for n_in not a positive multiple of 16, n_out not a positive multiple of 8, max_rows below 1; CF_EUNSUPPORTED for n_in above 131056,
  *   weights of 2 GiB or more, max_rows above 2^23.
