@@ -63,7 +63,7 @@ __global__ __launch_bounds__(T) void quantize_rows(const uint16_t *x, int8_t *co
 
 // ---- the product -------------------------------------------------------------------------------------------------------------
 //
-// 16 x 16 x 64 steps of the matrix units, 32-bit sums (exact: 2^31 / 127^2 codes and more).  Operands, lane = 16 g + c: row c, codes 16 g .. 16 g + 15.
+// 16 x 16 x 64 steps of the matrix units, 32-bit sums (exact below 2^31 / 128^2 = 131072 codes: kMostIn).  Operands, lane = 16 g + c: row c, codes 16 g .. 16 g + 15.
 struct LinearArgs {
     const int8_t *x, *w;
     const float *x_scale, *w_scale;
@@ -95,8 +95,10 @@ __device__ __forceinline__ void cf_lds_barrier() { asm volatile("s_waitcnt lgkmc
 // barrier holds up its loads.  (A lane of the matrix product holds a row, so that loads into registers would ask for 16 rows with every 16 lanes,
 // which passes 4.3 TB/s; into LDS eight adjacent lanes load 128 bytes of a row.)
 // Bound: memory where there are enough workgroups (1 x 4096 -> 12288: 50 MB in 11.4 us, of which some 2.5 are the launch; 4.9 TB/s while it streams),
-// else the requests that a compute unit has under way (1 x 28672 -> 1024, 64 workgroups: 16.4 us, with eight wavefronts 14.8; 64 x 4096 -> 6144,
-// 192 workgroups: 10.5 us).  Without gain: eight or sixteen wavefronts a workgroup (5.1 -> 6.0 us at 1 x 4096 -> 4096), rings in registers.
+// else the requests that a compute unit has under way (1 x 28672 -> 1024, 64 workgroups: 16.4 us; 64 x 4096 -> 6144, 192 workgroups: 10.5 us; all in
+// captured graphs, weights from memory).  Eight wavefronts a workgroup were faster at long sums of few outputs (the first of these 14.8 us) and slower at
+// ordinary ones (1 x 4096 -> 4096 5.1 -> 6.0): they are not among the ways, which do not know the length of the sum.  Without gain: sixteen
+// wavefronts, rings in registers.
 template <int MT, int NT, int WAVES, int DEPTH>
 __global__ __launch_bounds__(64 * WAVES) void linear_stream(const LinearArgs a)
 {
@@ -189,9 +191,9 @@ __global__ __launch_bounds__(64 * WAVES) void linear_stream(const LinearArgs a)
 // one that is used.  A row's eight 16-byte chunks lie there at places chunk ^ (row / 2 & 7), so that the rows of an operand are read from different banks
 // (chunk ^ (row & 7): every read from twice as many cycles); the loads fill LDS in the order of the lanes, so it is their addresses in memory that
 // are permuted.
-// Bound: the matrix units, and behind them the power that the card has for them: 8192 x 8192 -> 10240 in 604 us, 2.28 Pop/s, the units busy for 64 % of
-// the cycles at 1.7 GHz (a library's product of these sizes 647 us; the products alone, of operands that are not loaded, 475; the loads and the reading of
-// operands alone 396).  256 x 4096 -> 6144 takes 17.1 us, 512 x 4096 -> 4096 17.2: start, steps
+// Bound: the matrix units, and behind them the power that the card has for them: 8192 x 8192 -> 10240 in 604 to 618 us in a captured graph, 2.2 to 2.3 Pop/s,
+// the units busy for 64 % of the cycles at 1.7 GHz (called one by one 572 to 597 us, by card; in the graph a library's product of these sizes 647 us, the
+// products alone, of operands that are not loaded, 475, the loads and the reading of operands alone 396).  256 x 4096 -> 6144 takes 17.1 us, 512 x 4096 -> 4096 17.2: start, steps
 // and end of one tile on a compute unit.  Without gain: 128 x 128 to a wavefront, four on a compute unit (649 us); operands read where the compiler puts
 // them (618); the barrier and the next step's first operands before the last product of a step (609); through registers in place of direct loads (slower at all sizes).
 // Operands of a 32 x 32 x 32 step, lane = 32 g + c: row c, codes 16 g .. 16 g + 15; the result: output 8 (r / 4) + 4 g + r % 4 of row c.
@@ -306,7 +308,7 @@ constexpr Kernel kKernels[] = {            // of cf::linear::kWays
 static_assert(sizeof kKernels / sizeof *kKernels == cf::linear::kNumWays, "a kernel for each way");
 
 constexpr int kMostRows = 1 << 23;         // workgroups of a launch
-constexpr int kMostIn = 131056;            // 128^2 times as many is below 2^31
+constexpr int kMostIn = 131056;            // the last multiple of 16 that 128^2 times of is below 2^31: codes of -128 are allowed
 
 int check_linear(const cf_linear_config &c)
 {

@@ -1137,7 +1137,8 @@ __global__ __launch_bounds__(64 * RW * KG, 2) void tree_blocks(const TreeArgs a)
 // puts it as fp16 where the transposing reads of LDS find it, in its wavefront's own rows, so that no barrier is needed.
 // Bound: few rows as tree_tiles, by the chain of a step's loads (one token over 4096 rows, 32 heads, 10.7 us, 8.9 MB; over 32768 rows, 64 / 8 heads,
 // 15.5 us, 36 MB); many rows by the instructions of a step, 0.76 us of 32 rows x 32 keys x 128 dimensions on a SIMD: conversions, weights and products
-// take their turns there (64 tokens over 8192 rows, 32 / 8 heads, batch 16: 171 to 176 us, 0.8 PFLOP/s; tree_blocks with 4-bit staging the same).
+// take their turns there (64 tokens over 8192 rows, 32 / 8 heads, batch 16: 171 to 176 us, 0.8 PFLOP/s; tree_blocks with 4-bit staging the same; all
+// in captured graphs: called one by one that batch takes 161 to 167 us, by card).
 // Without gain: two or three steps of loads ahead in registers (1.4 us more in short calls: the code is larger) or in LDS, steps of 64 keys (long calls
 // -6 %, short ones +1 us), the next step's scores among this one's weights, 64 rows a wavefront (206 us), three wavefronts a SIMD (176), products of
 // 32 x 32 in place of 16 x 16 (184 against 171).
