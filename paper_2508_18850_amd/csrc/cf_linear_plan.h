@@ -9,7 +9,7 @@ namespace linear {
 // The ways to divide a product.  What a step of 128 codes of the sum takes a workgroup that has a compute unit for itself, and one among others on it, in
 // us; a call takes about 3 us more.  (Measured at 4096 to 11008 codes and 1 to 8192 rows, all ways at each; a wavefront of the tiles waits for its
 // operands and multiplies by turns, so that a step of a tile that is alone takes 1.5 times as long as the matrix units need for it or more.  The way that they
-// give takes up to 11 % longer than the best one at 18 shapes of 65 to 8192 rows and 512 to 12288 outputs: 256 x 4096 -> 6144 17.1 us, 15.4 in tiles of
+// give takes up to 7 % longer than the best one at 18 shapes of 65 to 8192 rows and 512 to 12288 outputs: 256 x 4096 -> 6144 16.5 us, 15.4 in tiles of
 // 64 x 64.  Under many rows with few outputs reading the rows counts, which they do not know: 4096 x 4096 -> 128 12.5 us, 10.3 in blocks of 64 x 64.)
 struct Way {
     int rows, cols, threads;       // of a workgroup
